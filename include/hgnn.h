@@ -53,6 +53,9 @@ typedef enum {
 
 enum { HGNN_F32 = 0, HGNN_BF16 = 1 };
 enum { HGNN_POOL_SUM = 0, HGNN_POOL_MEAN = 1 };
+enum { HGNN_NORM_RMS = 0, HGNN_NORM_LAYER = 1 };
+enum { HGNN_GATE_NONE = 0, HGNN_GATE_ATOM = 1, HGNN_GATE_CHANNEL = 2 };
+enum { HGNN_PAIR_NONE = 255 }; /* byte of a pair that is left out */
 enum { HGNN_ZMAX = 94 }; /* embedding table has HGNN_ZMAX+1 rows */
 
 const char* hgnn_last_error_string(void);
@@ -339,6 +342,61 @@ int32_t hgnn_multihead_deep_bwd(void* stream, int32_t N, int32_t G, int32_t H, i
                                 const float* g_energy /*[G]*/, const float* g_force /*[N,3]*/,
                                 float* g_p /*out [G,H]*/, float* g_h /*out [N,H]*/, float* g_v /*out [N,3]*/,
                                 float* gWhead /*out*/, void* ws, size_t ws_bytes);
+
+/* ---------------------------------------------------------------------------------------------
+ * Global attention blocks: beside the message passing between near atoms, a layer may let every atom of a structure attend to
+ * every other one (the paper's layers are local; such a block is put between or beside them). A block's own tensors are
+ * float32 with dtype HGNN_F32 and bfloat16 in memory with dtype HGNN_BF16 ("T" below); the residual stream, the parameters
+ * of norms, biases and every parameter gradient are float32. All of it accumulates in float32.
+ *
+ * hgnn_block_norm: the seam between two blocks -- closes one (norm after it, gate, residual scale, residual) and opens the
+ * next (norm before it):
+ *   x' = x + s * gamma * N(b; w1, c1),     y = N(x'; w0, c0),     N(u; w, c) = w * (u - mu) r + c per atom,
+ *   r = 1 / sqrt(mean((u - mu)^2) + eps),  mu = mean(u) (HGNN_NORM_LAYER) or 0 (HGNN_NORM_RMS),
+ *   gamma = 1 (HGNN_GATE_NONE), sigmoid(z) of one logit per atom, z [N] (HGNN_GATE_ATOM), or per channel, z [N,H].
+ * P is one flat float32 buffer s[H] w1[H] c1[H] w0[H] c0[H]; gP of _bwd has the same layout.
+ * b == NULL: nothing to close, y = N(x; w0, c0), x_out is not written (no gate then). y == NULL: nothing to open.
+ * `saved` (size from the query; NULL: no reverse pass follows) is written by _fwd and read by _bwd.
+ * _bwd takes x_out (x where b was NULL), g_x_out = dL/dx' past this seam's y (NULL = 0) and g_y (NULL where y was) and writes
+ * g_x, g_b, g_z and gP (zeros for what does not take part). x_out may alias x, g_x may alias g_x_out; no other aliasing.
+ * 1 <= H <= 1024. Errors: BAD_SHAPE for any other H, an unknown norm, gate or dtype, eps < 0, a gate without b.
+ * WORKSPACE_TOO_SMALL if ws or saved is smaller than the query says. Only enqueues work.
+ * ------------------------------------------------------------------------------------------- */
+int32_t hgnn_block_norm_workspace_bytes(int32_t N, int32_t H, size_t* ws_bytes_host, size_t* saved_bytes_host);
+int32_t hgnn_block_norm_fwd(void* stream, int32_t N, int32_t H, int32_t norm, int32_t gate, int32_t dtype, float eps,
+                            const float* x /*[N,H]*/, const void* b /*T [N,H] or NULL*/, const void* z /*T or NULL*/,
+                            const float* P /*[5,H]*/, float* x_out /*out [N,H]*/, void* y /*out T [N,H] or NULL*/,
+                            void* saved /*or NULL*/, size_t saved_bytes);
+int32_t hgnn_block_norm_bwd(void* stream, int32_t N, int32_t H, int32_t norm, int32_t gate, int32_t dtype,
+                            const float* x_out /*[N,H]*/, const void* b, const void* z, const float* P,
+                            const void* saved, size_t saved_bytes,
+                            const float* g_x_out /*[N,H] or NULL*/, const void* g_y /*T [N,H] or NULL*/,
+                            float* g_x /*out [N,H]*/, void* g_b /*out T [N,H]*/, void* g_z /*out T*/,
+                            float* gP /*out [5,H]*/, void* ws, size_t ws_bytes);
+
+/* ---------------------------------------------------------------------------------------------
+ * The pairs of atoms of each graph. A pair matrix holds one byte per ordered pair (i, j) of atoms of the same graph: graph
+ * g's n_g rows of pitch_g = n_g rounded up to 32 bytes, graph after graph; the bytes past a row's n_g-th are padding. A byte is
+ * the pair's bucket, or HGNN_PAIR_NONE for a pair that is left out.
+ * hgnn_pair_plan prepares a batch for the calls that work on pairs: plan is a device buffer of the queried size and belongs
+ * to this graph_off until the batch changes; *pair_bytes_host is the size of the pair matrix (sum of n_g pitch_g). It
+ * SYNCHRONISES the stream and returns BAD_OFFSETS if graph_off does not start at 0, decreases or does not end at N (a plan that
+ * was refused has no pair and no tile).
+ * hgnn_pair_buckets writes the matrix of distance buckets: the number of boundaries edge2[0..nedge) (ascending squares of
+ * lengths) that do not exceed d2, the smallest squared distance of i to the 27 images j + t of atom j,
+ *      t = (s1*a + s2*b) + s3*c, s in {-1,0,1}^3;  r = pos_i - (pos_j + t);  d2 = (rx*rx + ry*ry) + rz*rz
+ * in float32 with every operation rounded on its own (s = 0 alone where pbc[g] == 0, or cell or pbc is NULL). That is the
+ * nearest image of all for atoms inside a cell that is not very oblique. drop_far != 0: pairs beyond the last boundary become
+ * HGNN_PAIR_NONE. Padding becomes HGNN_PAIR_NONE. 0 <= nedge <= 254. A matrix may as well be filled by the caller (hops along
+ * bonds, say). Only enqueues work; deterministic to the bit.
+ * N and G below 2^28 (else OVERFLOW).
+ * ------------------------------------------------------------------------------------------- */
+int32_t hgnn_pair_plan_workspace_bytes(int32_t N, int32_t G, size_t* plan_bytes_host);
+int32_t hgnn_pair_plan(void* stream, int32_t N, int32_t G, const int32_t* graph_off /*[G+1]*/, void* plan /*out*/,
+                       size_t plan_bytes, int64_t* pair_bytes_host /*out, host*/);
+int32_t hgnn_pair_buckets(void* stream, int32_t N, int32_t G, const void* plan, size_t plan_bytes, const float* pos /*[N,3]*/,
+                          const float* cell /*[G,3,3] or NULL*/, const uint8_t* pbc /*[G] or NULL*/,
+                          int32_t nedge, const float* edge2 /*[nedge]*/, int32_t drop_far, uint8_t* pairs /*out*/);
 
 /* ---------------------------------------------------------------------------------------------
  * AdamW update of a flat float32 parameter buffer (paper, training setup: the optimiser is AdamW, learning rate 1e-3;

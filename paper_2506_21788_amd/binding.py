@@ -16,6 +16,9 @@ LIB_PATH = os.path.join(_HERE, "libhgnn.so")
 
 F32, BF16 = 0, 1
 POOL_SUM, POOL_MEAN = 0, 1
+NORM_RMS, NORM_LAYER = 0, 1
+GATE_NONE, GATE_ATOM, GATE_CHANNEL = 0, 1, 2
+PAIR_NONE = 255
 ZMAX = 94
 
 EXPORTS = [
@@ -29,6 +32,8 @@ EXPORTS = [
     "hgnn_multihead_plan_ints", "hgnn_multihead_plan",
     "hgnn_multihead_decode_workspace_bytes", "hgnn_multihead_decode_fwd", "hgnn_multihead_decode_bwd",
     "hgnn_multihead_deep_workspace_bytes", "hgnn_multihead_deep_fwd", "hgnn_multihead_deep_bwd",
+    "hgnn_block_norm_workspace_bytes", "hgnn_block_norm_fwd", "hgnn_block_norm_bwd",
+    "hgnn_pair_plan_workspace_bytes", "hgnn_pair_plan", "hgnn_pair_buckets",
     "hgnn_adamw_step",
     "hgnn_profile_begin", "hgnn_profile_end", "hgnn_profile_num_tags", "hgnn_profile_tag_name",
     "hgnn_profile_read",
@@ -74,6 +79,8 @@ _mp_ws = _sig("hgnn_mp_layer_workspace_bytes", i32, i64, i32, i32, C.POINTER(sz)
 _mpa_ws = _sig("hgnn_mp_layer_attr_workspace_bytes", i32, i64, i32, i32, i32, C.POINTER(sz), C.POINTER(sz))
 _dec_ws = _sig("hgnn_multihead_decode_workspace_bytes", i32, i32, i32, i32, i32, i32, C.POINTER(sz), C.POINTER(sz))
 _deep_ws = _sig("hgnn_multihead_deep_workspace_bytes", i32, i32, i32, i32, i32, i32, i32, C.POINTER(sz), C.POINTER(sz))
+_norm_ws = _sig("hgnn_block_norm_workspace_bytes", i32, i32, C.POINTER(sz), C.POINTER(sz))
+_pair_ws = _sig("hgnn_pair_plan_workspace_bytes", i32, i32, C.POINTER(sz))
 
 
 def last_error_string() -> str:
@@ -247,6 +254,38 @@ def multihead_deep_bwd(N, G, H, Hh, D, S, dtype, plan, p, h, v, Whead, saved, g_
                        gWhead, ws):
     _check(_n.multihead_deep_bwd(N, G, H, Hh, D, S, dtype, plan, p, h, v, Whead, saved, g_energy, g_force, g_p, g_h,
                                  g_v, gWhead, ws))
+
+
+def block_norm_workspace_bytes(N, H):
+    a, b = sz(0), sz(0)
+    _check(_norm_ws(N, H, C.byref(a), C.byref(b)))
+    return a.value, b.value
+
+
+def block_norm_fwd(N, H, norm, gate, dtype, eps, x, b, z, P, x_out, y, saved):
+    _check(_n.block_norm_fwd(N, H, norm, gate, dtype, eps, x, b, z, P, x_out, y, saved))
+
+
+def block_norm_bwd(N, H, norm, gate, dtype, x_out, b, z, P, saved, g_x_out, g_y, g_x, g_b, g_z, gP, ws):
+    _check(_n.block_norm_bwd(N, H, norm, gate, dtype, x_out, b, z, P, saved, g_x_out, g_y, g_x, g_b, g_z, gP, ws))
+
+
+def pair_plan_workspace_bytes(N, G):
+    b = sz(0)
+    _check(_pair_ws(N, G, C.byref(b)))
+    return b.value
+
+
+def pair_plan(N, G, graph_off, plan):
+    """Fills `plan` (a uint8 tensor) and returns the bytes of the pair matrix."""
+    size = _n.pair_plan(N, G, graph_off, plan)
+    if size < 0:
+        _check(size)
+    return size
+
+
+def pair_buckets(N, G, plan, pos, cell, pbc, nedge, edge2, drop_far, pairs):
+    _check(_n.pair_buckets(N, G, plan, pos, cell, pbc, nedge, edge2, int(drop_far), pairs))
 
 
 # ------------------------------------------------------------------------------------------------

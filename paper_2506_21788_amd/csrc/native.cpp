@@ -112,6 +112,16 @@ PyObject* call_count(PyObject*, PyObject* const* v, Py_ssize_t n) {
   int64_t E = 0;
   return run(&count_edges, v, n, E) ? PyLong_FromLongLong(E) : nullptr;
 }
+// the bytes of the pair matrix, or the code
+int64_t plan_pairs(void* st, int32_t N, int32_t G, const int32_t* graph_off, void* plan, size_t plan_bytes) {
+  int64_t bytes = 0;
+  const int32_t code = hgnn_pair_plan(st, N, G, graph_off, plan, plan_bytes, &bytes);
+  return code != HGNN_OK ? code : bytes;
+}
+PyObject* call_pair_plan(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  int64_t bytes = 0;
+  return run(&plan_pairs, v, n, bytes) ? PyLong_FromLongLong(bytes) : nullptr;
+}
 
 #define ENTRY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call<&hgnn_##name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
@@ -123,6 +133,9 @@ PyMethodDef methods[] = {
     ENTRY(pool_by_graph_fwd), ENTRY(pool_by_graph_bwd),
     ENTRY(multihead_plan), ENTRY(multihead_decode_fwd), ENTRY(multihead_decode_bwd),
     ENTRY(multihead_deep_fwd), ENTRY(multihead_deep_bwd),
+    ENTRY(block_norm_fwd), ENTRY(block_norm_bwd),
+    {"pair_plan", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call_pair_plan)), METH_FASTCALL, nullptr},
+    ENTRY(pair_buckets),
     ENTRY(adamw_step),
     {nullptr, nullptr, 0, nullptr},
 };

@@ -1,0 +1,220 @@
+// hgnn_pair_plan and hgnn_pair_buckets: the matrix of distance buckets of every graph, one byte a pair.
+//
+// The distance is that of the nearest of the 27 images j + t, t = (s1 a + s2 b) + s3 c with s in {-1, 0, 1}^3, each formed in
+// float32 with every operation rounded on its own (this file is compiled without contraction), so the bytes do not depend
+// on how the work is cut: a minimum over values has no ties to break. 12 operations an image and pair, 324 a pair in a
+// periodic graph and 12 otherwise, against one byte written: bound by the vector units. A thread takes four neighbouring pairs
+// of a row (one 4-byte store), a workgroup eight rows, whose positions and images stay in registers and shared memory.
+#include "common.h"
+#include "pairs.h"
+#include "prof.h"
+
+namespace hgnn {
+namespace {
+
+constexpr int PAIR_EDGES = 254;   // most boundaries: buckets 0..254, byte 255 is HGNN_PAIR_NONE
+
+// one workgroup: running sums over the graphs, the check of the offsets, the total for the host
+__global__ void __launch_bounds__(1024) k_pair_plan(int N, int G, const int32_t* graph_off, PairPlan v, HostMail* mail) {
+  __shared__ long long wb[16];
+  __shared__ int wt[16], bad_s;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (tid == 0) bad_s = 0;
+  __syncthreads();
+  long long base_b = 0;
+  int base_t = 0;
+  int bad = 0;
+  if (tid == 0) bad = graph_off[0] != 0 || graph_off[G] != N;
+  for (int g0 = 0; g0 < G; g0 += 1024) {
+    const int g = g0 + tid;
+    long long bytes = 0;
+    int tiles = 0;
+    if (g < G) {
+      const int lo = graph_off[g], hi = graph_off[g + 1];
+      if (lo < 0 || hi < lo || hi > N) bad = 1;
+      else {
+        const long long n = hi - lo;
+        bytes = n * pair_pitch(n);
+        tiles = (int)((n + PAIR_T - 1) / PAIR_T);
+      }
+    }
+    long long ib = bytes;
+    int it = tiles;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const long long ub = __shfl_up(ib, d);
+      const int ut = __shfl_up(it, d);
+      if (lane >= d) { ib += ub; it += ut; }
+    }
+    if (lane == 63) { wb[wave] = ib; wt[wave] = it; }
+    __syncthreads();
+    long long pb = base_b, tb = 0;
+    int pt = base_t, tt = 0;
+    for (int w = 0; w < 16; ++w) {
+      if (w < wave) { pb += wb[w]; pt += wt[w]; }
+      tb += wb[w];
+      tt += wt[w];
+    }
+    if (g < G) {
+      v.pair_off[g] = pb + ib - bytes;
+      v.tile_off[g] = pt + it - tiles;
+      v.graph_off[g] = graph_off[g];
+    }
+    base_b += tb;
+    base_t += tt;
+    __syncthreads();
+  }
+  if (bad) atomicOr(&bad_s, 1);
+  __syncthreads();
+  if (tid == 0) {
+    v.pair_off[G] = bad_s ? 0 : base_b;
+    v.graph_off[G] = N;
+    v.tile_off[G] = bad_s ? 0 : base_t;
+    post_mail(mail, base_b, bad_s);
+  }
+}
+
+// the graph of every tile: a binary search per tile
+__global__ void __launch_bounds__(256) k_pair_tiles(int G, PairPlan v) {
+  const int t = blockIdx.x * 256 + threadIdx.x;
+  if (t >= v.tile_off[G]) return;
+  int lo = 0, hi = G;   // tile_off[lo] <= t < tile_off[hi]
+  while (hi - lo > 1) {
+    const int m = (lo + hi) >> 1;
+    if (v.tile_off[m] <= t) lo = m;
+    else hi = m;
+  }
+  v.tile_graph[t] = lo;
+}
+
+struct BucketArgs {
+  int G, nedge, drop_far;
+  const float *pos, *cell, *edge2;
+  const uint8_t* pbc;
+  PairPlan plan;
+  uint8_t* pairs;
+};
+
+// workgroup: 8 rows of a tile; thread: row tid / 32, pairs 4 (tid % 32) .. + 3 of every 128
+__global__ void __launch_bounds__(256) k_pair_buckets(BucketArgs a) {
+  __shared__ float4 img[27];
+  __shared__ float edge[PAIR_EDGES + 1];
+  const int tile = blockIdx.x >> 2;
+  if (tile >= a.plan.tile_off[a.G]) return;
+  const int g = a.plan.tile_graph[tile];
+  const int lo = a.plan.graph_off[g], n = a.plan.graph_off[g + 1] - lo;
+  const int i0 = (tile - a.plan.tile_off[g]) * PAIR_T + (blockIdx.x & 3) * 8;
+  if (i0 >= n) return;
+  const bool periodic = a.cell && a.pbc && a.pbc[g];
+  if (threadIdx.x < 27) {
+    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (periodic) {
+      const float s1 = (int)threadIdx.x / 9 - 1, s2 = (int)threadIdx.x / 3 % 3 - 1, s3 = (int)threadIdx.x % 3 - 1;
+      const float* c = a.cell + (size_t)g * 9;
+      t.x = (s1 * c[0] + s2 * c[3]) + s3 * c[6];
+      t.y = (s1 * c[1] + s2 * c[4]) + s3 * c[7];
+      t.z = (s1 * c[2] + s2 * c[5]) + s3 * c[8];
+    }
+    img[threadIdx.x] = t;
+  }
+  for (int e = threadIdx.x; e < a.nedge; e += 256) edge[e] = a.edge2[e];
+  __syncthreads();
+  const int i = i0 + (threadIdx.x >> 5);
+  if (i >= n) return;
+  const float* p = a.pos + ((size_t)lo + i) * 3;
+  const float px = p[0], py = p[1], pz = p[2];
+  const int64_t pitch = pair_pitch(n);
+  uint8_t* row = a.pairs + a.plan.pair_off[g] + i * pitch;
+  const int first = periodic ? 0 : 13, last = periodic ? 26 : 13;
+  for (int j = (threadIdx.x & 31) * 4; j < pitch; j += 128) {
+    float q[4][3], best[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int jj = j + k < n ? j + k : n - 1;
+      const float* s = a.pos + ((size_t)lo + jj) * 3;
+      q[k][0] = s[0]; q[k][1] = s[1]; q[k][2] = s[2];
+      best[k] = __builtin_inff();
+    }
+    for (int m = first; m <= last; ++m) {
+      const float4 t = img[m];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float x = px - (q[k][0] + t.x), y = py - (q[k][1] + t.y), z = pz - (q[k][2] + t.z);
+        best[k] = fminf(best[k], (x * x + y * y) + z * z);
+      }
+    }
+    unsigned out = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      int lo_e = 0, hi_e = a.nedge;   // boundaries below lo_e are <= best, boundaries from hi_e on are above it
+      while (lo_e < hi_e) {
+        const int m = (lo_e + hi_e) >> 1;
+        if (best[k] < edge[m]) hi_e = m;
+        else lo_e = m + 1;
+      }
+      const unsigned b = j + k >= n || (a.drop_far && lo_e == a.nedge) ? (unsigned)HGNN_PAIR_NONE : (unsigned)lo_e;
+      out |= b << (8 * k);
+    }
+    *reinterpret_cast<unsigned*>(row + j) = out;
+  }
+}
+
+}  // namespace
+}  // namespace hgnn
+
+using namespace hgnn;
+
+static int32_t check_pair(int32_t N, int32_t G) {
+  HGNN_REQUIRE(N >= 0 && G >= 0, HGNN_ERR_BAD_SHAPE, "negative N or G");
+  HGNN_REQUIRE(N < (1 << 28) && G < (1 << 28), HGNN_ERR_OVERFLOW, "pair matrix: N and G must be below 2^28");
+  return HGNN_OK;
+}
+
+extern "C" int32_t hgnn_pair_plan_workspace_bytes(int32_t N, int32_t G, size_t* plan_bytes_host) {
+  HGNN_TRY(check_pair(N, G));
+  HGNN_REQUIRE(plan_bytes_host, HGNN_ERR_NULLPTR, "null size pointer");
+  *plan_bytes_host = pair_plan_view(nullptr, N, G).bytes;
+  return HGNN_OK;
+}
+
+extern "C" int32_t hgnn_pair_plan(void* stream, int32_t N, int32_t G, const int32_t* graph_off, void* plan, size_t plan_bytes,
+                                  int64_t* pair_bytes_host) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  HGNN_TRY(check_pair(N, G));
+  HGNN_REQUIRE(graph_off && plan && pair_bytes_host, HGNN_ERR_NULLPTR, "pair_plan: null pointer");
+  const PairPlan v = pair_plan_view(plan, N, G);
+  HGNN_REQUIRE(plan_bytes >= v.bytes, HGNN_ERR_WORKSPACE_TOO_SMALL, "pair plan: need %zu bytes, got %zu", v.bytes, plan_bytes);
+  MailSlot mail;
+  HGNN_TRY(mail.take(st));
+  {
+    ProfScope ps(PT_MISC, st);
+    k_pair_plan<<<1, 1024, 0, st>>>(N, G, graph_off, v, mail.dev());
+    HGNN_LAUNCH_CHECK("k_pair_plan");
+    if (v.max_tiles > 0) {
+      k_pair_tiles<<<(unsigned)((v.max_tiles + 255) / 256), 256, 0, st>>>(G, v);
+      HGNN_LAUNCH_CHECK("k_pair_tiles");
+    }
+  }
+  HGNN_HIP(mail.wait());
+  HGNN_REQUIRE(mail.status() == 0, HGNN_ERR_BAD_OFFSETS, "graph_off must start at 0, not decrease and end at N");
+  *pair_bytes_host = mail.value();
+  return HGNN_OK;
+}
+
+extern "C" int32_t hgnn_pair_buckets(void* stream, int32_t N, int32_t G, const void* plan, size_t plan_bytes, const float* pos,
+                                     const float* cell, const uint8_t* pbc, int32_t nedge, const float* edge2,
+                                     int32_t drop_far, uint8_t* pairs) {
+  HGNN_TRY(check_pair(N, G));
+  HGNN_REQUIRE(nedge >= 0 && nedge <= PAIR_EDGES, HGNN_ERR_BAD_SHAPE, "pair_buckets: 0..%d boundaries (got %d)", PAIR_EDGES, nedge);
+  if (N == 0) return HGNN_OK;
+  HGNN_REQUIRE(plan && pos && pairs && (edge2 || nedge == 0), HGNN_ERR_NULLPTR, "pair_buckets: null pointer");
+  BucketArgs a{};
+  a.plan = pair_plan_view(plan, N, G);
+  HGNN_REQUIRE(plan_bytes >= a.plan.bytes, HGNN_ERR_WORKSPACE_TOO_SMALL, "pair plan: need %zu bytes, got %zu", a.plan.bytes, plan_bytes);
+  a.G = G; a.nedge = nedge; a.drop_far = drop_far; a.pos = pos; a.cell = cell; a.edge2 = edge2; a.pbc = pbc; a.pairs = pairs;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  ProfScope ps(PT_MISC, st);
+  k_pair_buckets<<<(unsigned)(a.plan.max_tiles * 4), 256, 0, st>>>(a);
+  HGNN_LAUNCH_CHECK("k_pair_buckets");
+  return HGNN_OK;
+}

@@ -1,0 +1,55 @@
+"""Refusals of the attention block's entry points: found on the host, before any launch (no GPU needed)."""
+import ctypes
+import os
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LIB = os.path.join(ROOT, "paper_2506_21788_amd", "libhgnn.so")
+NULL, SHAPE, WS, OVERFLOW = -1, -2, -6, -7
+i32, i64, f32, vp, sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t
+P = vp(0x1000)      # never dereferenced
+
+
+def _lib():
+    lib = ctypes.CDLL(LIB)
+    lib.hgnn_last_error_string.restype = ctypes.c_char_p
+    return lib
+
+
+def test_block_norm():
+    lib = _lib()
+    a, b = sz(0), sz(0)
+    size = lambda N, H: lib.hgnn_block_norm_workspace_bytes(i32(N), i32(H), ctypes.byref(a), ctypes.byref(b))  # noqa: E731
+    assert size(10, 1024) == 0 and b.value == 160 and size(0, 1) == 0
+    assert size(10, 1025) == SHAPE and size(10, 0) == SHAPE and size(-1, 4) == SHAPE
+    assert lib.hgnn_block_norm_workspace_bytes(i32(1), i32(1), None, ctypes.byref(b)) == NULL
+
+    def fwd(N=4, H=8, norm=0, gate=0, dt=0, eps=1e-5, x=P, blk=P, z=None, par=P, xo=P, y=P, saved=None, sb=0):
+        return lib.hgnn_block_norm_fwd(None, i32(N), i32(H), i32(norm), i32(gate), i32(dt), f32(eps), x, blk, z, par, xo, y, saved, sz(sb))
+    for kw, code in ((dict(norm=2), SHAPE), (dict(gate=3), SHAPE), (dict(dt=2), SHAPE), (dict(eps=-1.0), SHAPE), (dict(eps=float("nan")), SHAPE),
+                     (dict(blk=None, gate=1, z=P), SHAPE), (dict(gate=2), NULL), (dict(x=None), NULL), (dict(par=None), NULL),
+                     (dict(xo=None), NULL), (dict(blk=None, y=None), NULL), (dict(saved=P, sb=63), WS), (dict(N=0, x=None), 0)):
+        assert fwd(**kw) == code, kw
+
+    def bwd(N=4, H=8, gate=0, xo=P, blk=P, z=None, saved=P, sb=64, gxo=P, gy=P, gx=P, gb=P, gz=None, gP=P, ws=P, wb=1 << 20):
+        return lib.hgnn_block_norm_bwd(None, i32(N), i32(H), i32(0), i32(gate), i32(0), xo, blk, z, P, saved, sz(sb), gxo, gy, gx, gb, gz, gP,
+                                       ws, sz(wb))
+    for kw, code in ((dict(wb=8), WS), (dict(sb=63), WS), (dict(gP=None), NULL), (dict(gxo=None, gy=None), NULL), (dict(xo=None), NULL),
+                     (dict(gb=None), NULL), (dict(gate=1, z=P), NULL), (dict(gate=1, gz=P), NULL), (dict(saved=None), NULL), (dict(H=2000), SHAPE)):
+        assert bwd(**kw) == code, kw
+
+
+def test_pairs():
+    lib = _lib()
+    a = sz(0)
+    size = lambda N, G: lib.hgnn_pair_plan_workspace_bytes(i32(N), i32(G), ctypes.byref(a))  # noqa: E731
+    assert size(0, 0) == 0 and size(1000, 10) == 0 and a.value > 12 * 11
+    assert size(-1, 1) == SHAPE and size(1, -1) == SHAPE and size(1 << 28, 1) == OVERFLOW and size(1, 1 << 28) == OVERFLOW
+    out = i64(0)
+    plan = lambda off=P, p=P, pb=1 << 20, o=ctypes.byref(out): lib.hgnn_pair_plan(None, i32(5), i32(1), off, p, sz(pb), o)  # noqa: E731
+    assert plan(off=None) == NULL and plan(p=None) == NULL and plan(o=None) == NULL and plan(pb=8) == WS
+
+    def buckets(N=5, p=P, pb=1 << 20, pos=P, ne=3, e=P, m=P):
+        return lib.hgnn_pair_buckets(None, i32(N), i32(1), p, sz(pb), pos, None, None, i32(ne), e, i32(0), m)
+    for kw, code in ((dict(ne=-1), SHAPE), (dict(ne=255), SHAPE), (dict(p=None), NULL), (dict(pos=None), NULL), (dict(e=None), NULL),
+                     (dict(m=None), NULL), (dict(pb=8), WS), (dict(N=-1), SHAPE), (dict(N=0, pos=None), 0)):
+        assert buckets(**kw) == code, kw

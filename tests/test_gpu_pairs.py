@@ -1,0 +1,66 @@
+"""Pair plans and distance buckets: byte for byte against the float32 form on the host (needs a GPU)."""
+import numpy as np
+import pytest
+
+from block_util import dev, room, untouched
+from oracle import block as ob
+
+pytestmark = pytest.mark.gpu
+
+
+def _sizes(kind):
+    return {"none": [], "one": [1], "empty ends": [0, 3, 0, 0, 33, 0], "edges": [31, 32, 33, 64, 65, 127, 1, 128],
+            "many": [(7 * i) % 23 for i in range(3000)], "long": [1111]}[kind]
+
+
+@pytest.mark.parametrize("kind", ["none", "one", "empty ends", "edges", "many", "long"])
+@pytest.mark.parametrize("nedge,drop", [(0, False), (1, True), (31, False), (254, True)])
+def test_buckets(kind, nedge, drop):
+    import torch
+    from paper_2506_21788_amd import binding as B
+    n = np.array(_sizes(kind), np.int64)
+    if kind in ("many", "long") and nedge not in (1, 31):
+        pytest.skip("the small batches cover it")
+    print("pair_buckets", kind, nedge, drop, flush=True)
+    rng = np.random.default_rng(len(n) + nedge)
+    off = np.concatenate([[0], np.cumsum(n)]).astype(np.int32)
+    N, G = int(off[-1]), len(n)
+    cell = (6 * np.eye(3) + 2 * rng.standard_normal((G, 3, 3)) * 0.5).astype(np.float32)
+    frac = rng.random((N, 3))
+    frac[::5] = np.round(frac[::5] * 2) / 2            # ties between images
+    pos = np.einsum("na,nab->nb", frac, cell[np.repeat(np.arange(G), n)].astype(np.float64)).astype(np.float32)
+    if N > 3:
+        pos[3] = pos[1]                                # two atoms in one place
+    pbc = (np.arange(G) % 2).astype(np.uint8)
+    edge2 = np.sort(rng.random(nedge) * 6).astype(np.float32) ** 2
+    plan = torch.empty(B.pair_plan_workspace_bytes(N, G), dtype=torch.uint8, device="cuda")
+    size = B.pair_plan(N, G, dev(off, "i32"), plan)
+    assert size == ob.pair_layout(off)[0][-1]
+    for c, p in ((cell, pbc), (None, pbc), (cell, None)):
+        got, guard = room(size)
+        B.pair_buckets(N, G, plan, dev(pos), dev(c), dev(p, "u8"), nedge, dev(edge2), drop, got)
+        assert np.array_equal(got.cpu().numpy(), ob.pair_buckets(pos, off, c, p, edge2, drop)) and untouched(guard)
+
+
+def test_distance_that_is_no_number_is_beyond_every_boundary():
+    import torch
+    from paper_2506_21788_amd import binding as B
+    pos = torch.tensor([[0.0, 0, 0], [float("nan"), 0, 0], [float("inf"), 0, 0]], device="cuda")
+    plan = torch.empty(B.pair_plan_workspace_bytes(3, 1), dtype=torch.uint8, device="cuda")
+    m = torch.empty(B.pair_plan(3, 1, dev(np.array([0, 3]), "i32"), plan), dtype=torch.uint8, device="cuda")
+    B.pair_buckets(3, 1, plan, pos, None, None, 2, dev(np.array([1.0, 4.0])), False, m)
+    assert m.view(3, 32)[:, :3].tolist() == [[0, 2, 2], [2, 2, 2], [2, 2, 2]]
+
+
+@pytest.mark.parametrize("off", [[1, 5], [0, 4], [0, 6], [0, 3, 2, 5], [0, -1, 5], [0, 9, 5]])
+def test_bad_offsets_are_found_and_leave_an_empty_plan(off):
+    import torch
+    from paper_2506_21788_amd import binding as B
+    N, G = 5, len(off) - 1
+    plan = torch.empty(B.pair_plan_workspace_bytes(N, G), dtype=torch.uint8, device="cuda")
+    with pytest.raises(B.HgnnError) as e:
+        B.pair_plan(N, G, dev(np.array(off), "i32"), plan)
+    assert e.value.code == -3
+    m = torch.full((512,), 7, dtype=torch.uint8, device="cuda")
+    B.pair_buckets(N, G, plan, torch.zeros((N, 3), device="cuda"), None, None, 1, torch.ones(1, device="cuda"), False, m)
+    assert bool((m == 7).all())
