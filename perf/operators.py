@@ -338,7 +338,7 @@ def _own_attention(s):
         return k
 
     k = _buf(s, make)
-    B.graph_attention_fwd(N, G, h, kv, d, nb, dtype, s.scale, k.plan, s.pairs, s.qkv, s.bias, k.out, k.saved, k.ws)
+    B.graph_attention_fwd(N, G, h, kv, d, nb, dtype, s.scale, k.plan, s.pairs, s.qkv, s.bias, k.out, k.saved)
     if not c["train"]:
         return {"out": k.out}
     B.graph_attention_bwd(N, G, h, kv, d, nb, dtype, s.scale, k.plan, s.pairs, s.qkv, s.bias, k.out, k.saved, s.g_out, k.g_qkv,
