@@ -26,7 +26,7 @@
  *  - dtype selects the GEMM operand type: HGNN_F32 (fp32 matrix cores) or HGNN_BF16 (operands rounded
  *    to bf16 on load, fp32 accumulation). Activations, aggregation, biases and SiLU stay fp32.
  *  - Gradient outputs are overwritten, not accumulated, unless said otherwise.
- *  - Results are deterministic: no floating-point atomics anywhere, all reductions in a fixed order.
+ *  - Results are deterministic: no two threads add to one floating-point word, all reductions in a fixed order.
  */
 #ifndef HGNN_H
 #define HGNN_H
@@ -397,6 +397,32 @@ int32_t hgnn_pair_plan(void* stream, int32_t N, int32_t G, const int32_t* graph_
 int32_t hgnn_pair_buckets(void* stream, int32_t N, int32_t G, const void* plan, size_t plan_bytes, const float* pos /*[N,3]*/,
                           const float* cell /*[G,3,3] or NULL*/, const uint8_t* pbc /*[G] or NULL*/,
                           int32_t nedge, const float* edge2 /*[nedge]*/, int32_t drop_far, uint8_t* pairs /*out*/);
+
+/* ---------------------------------------------------------------------------------------------
+ * Attention over the atoms of each graph, with a learned bias per head and pair bucket:
+ *   s_ij = scale q_i . k_j + bias[h][bucket_ij]   over the atoms j of i's graph whose pair byte is below nb,
+ *   out_i = sum_j softmax_j(s)_ij v_j
+ * qkv is T [N, nh + 2 nkv, dh]: nh query heads, nkv key heads, nkv value heads; query head h reads key and value head
+ * h / (nh / nkv). out is T [N, nh, dh], bias float32 [nh, nb]; g_qkv and g_bias have the layouts of qkv and bias. A pair whose byte is
+ * nb or more, or whose bias is -inf, is left out: its atoms may hold anything, infinities and NaN too. (Such values are slow:
+ * a tile of 32 rows whose result is not finite is formed again pair by pair.) A row without pairs gives zeros and zero gradients.
+ * Buckets have no gradient with respect to positions.
+ * `saved` (NULL: no reverse pass follows) is written by _fwd and read by _bwd with the same out. plan: hgnn_pair_plan of this
+ * batch; pairs: a pair matrix of it (its padding is not looked at).
+ * 1 <= nh <= 64, nkv divides nh, dh a multiple of 8 in 8..128, 1 <= nb <= 64 (else BAD_SHAPE). N and G below 2^28, and
+ * (N / 32 + min(N, G) + 64) nh below 2^31 (else OVERFLOW). Only enqueue work.
+ * dtype HGNN_BF16 rounds p and ds to bfloat16 where they enter the products of g_q, g_k and g_v; out, g_bias and all softmax
+ * statistics are formed without such a rounding.
+ * ------------------------------------------------------------------------------------------- */
+int32_t hgnn_graph_attention_workspace_bytes(int32_t N, int32_t G, int32_t nh, int32_t nkv, int32_t dh, int32_t nb, int32_t dtype,
+                                             size_t* ws_bytes_host, size_t* saved_bytes_host);
+int32_t hgnn_graph_attention_fwd(void* stream, int32_t N, int32_t G, int32_t nh, int32_t nkv, int32_t dh, int32_t nb, int32_t dtype,
+                                 float scale, const void* plan, size_t plan_bytes, const uint8_t* pairs,
+                                 const void* qkv, const float* bias, void* out /*out*/, void* saved /*or NULL*/, size_t saved_bytes);
+int32_t hgnn_graph_attention_bwd(void* stream, int32_t N, int32_t G, int32_t nh, int32_t nkv, int32_t dh, int32_t nb, int32_t dtype,
+                                 float scale, const void* plan, size_t plan_bytes, const uint8_t* pairs,
+                                 const void* qkv, const float* bias, const void* out, const void* saved, size_t saved_bytes,
+                                 const void* g_out, void* g_qkv /*out*/, float* g_bias /*out*/, void* ws, size_t ws_bytes);
 
 /* ---------------------------------------------------------------------------------------------
  * AdamW update of a flat float32 parameter buffer (paper, training setup: the optimiser is AdamW, learning rate 1e-3;

@@ -34,6 +34,7 @@ EXPORTS = [
     "hgnn_multihead_deep_workspace_bytes", "hgnn_multihead_deep_fwd", "hgnn_multihead_deep_bwd",
     "hgnn_block_norm_workspace_bytes", "hgnn_block_norm_fwd", "hgnn_block_norm_bwd",
     "hgnn_pair_plan_workspace_bytes", "hgnn_pair_plan", "hgnn_pair_buckets",
+    "hgnn_graph_attention_workspace_bytes", "hgnn_graph_attention_fwd", "hgnn_graph_attention_bwd",
     "hgnn_adamw_step",
     "hgnn_profile_begin", "hgnn_profile_end", "hgnn_profile_num_tags", "hgnn_profile_tag_name",
     "hgnn_profile_read",
@@ -81,6 +82,7 @@ _dec_ws = _sig("hgnn_multihead_decode_workspace_bytes", i32, i32, i32, i32, i32,
 _deep_ws = _sig("hgnn_multihead_deep_workspace_bytes", i32, i32, i32, i32, i32, i32, i32, C.POINTER(sz), C.POINTER(sz))
 _norm_ws = _sig("hgnn_block_norm_workspace_bytes", i32, i32, C.POINTER(sz), C.POINTER(sz))
 _pair_ws = _sig("hgnn_pair_plan_workspace_bytes", i32, i32, C.POINTER(sz))
+_attn_ws = _sig("hgnn_graph_attention_workspace_bytes", i32, i32, i32, i32, i32, i32, i32, C.POINTER(sz), C.POINTER(sz))
 
 
 def last_error_string() -> str:
@@ -286,6 +288,22 @@ def pair_plan(N, G, graph_off, plan):
 
 def pair_buckets(N, G, plan, pos, cell, pbc, nedge, edge2, drop_far, pairs):
     _check(_n.pair_buckets(N, G, plan, pos, cell, pbc, nedge, edge2, int(drop_far), pairs))
+
+
+def graph_attention_workspace_bytes(N, G, heads, kv_heads, head_dim, buckets, dtype):
+    a, b = sz(0), sz(0)
+    _check(_attn_ws(N, G, heads, kv_heads, head_dim, buckets, dtype, C.byref(a), C.byref(b)))
+    return a.value, b.value
+
+
+def graph_attention_fwd(N, G, heads, kv_heads, head_dim, buckets, dtype, scale, plan, pairs, qkv, bias, out, saved):
+    _check(_n.graph_attention_fwd(N, G, heads, kv_heads, head_dim, buckets, dtype, scale, plan, pairs, qkv, bias, out, saved))
+
+
+def graph_attention_bwd(N, G, heads, kv_heads, head_dim, buckets, dtype, scale, plan, pairs, qkv, bias, out, saved, g_out, g_qkv,
+                        g_bias, ws):
+    _check(_n.graph_attention_bwd(N, G, heads, kv_heads, head_dim, buckets, dtype, scale, plan, pairs, qkv, bias, out, saved, g_out,
+                                  g_qkv, g_bias, ws))
 
 
 # ------------------------------------------------------------------------------------------------

@@ -135,7 +135,7 @@ PyMethodDef methods[] = {
     ENTRY(multihead_deep_fwd), ENTRY(multihead_deep_bwd),
     ENTRY(block_norm_fwd), ENTRY(block_norm_bwd),
     {"pair_plan", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call_pair_plan)), METH_FASTCALL, nullptr},
-    ENTRY(pair_buckets),
+    ENTRY(pair_buckets), ENTRY(graph_attention_fwd), ENTRY(graph_attention_bwd),
     ENTRY(adamw_step),
     {nullptr, nullptr, 0, nullptr},
 };

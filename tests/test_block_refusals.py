@@ -53,3 +53,30 @@ def test_pairs():
     for kw, code in ((dict(ne=-1), SHAPE), (dict(ne=255), SHAPE), (dict(p=None), NULL), (dict(pos=None), NULL), (dict(e=None), NULL),
                      (dict(m=None), NULL), (dict(pb=8), WS), (dict(N=-1), SHAPE), (dict(N=0, pos=None), 0)):
         assert buckets(**kw) == code, kw
+
+
+def test_graph_attention():
+    lib = _lib()
+    a, b = sz(0), sz(0)
+
+    def size(N=100, G=3, nh=4, kv=2, d=32, nb=8, dt=0):
+        return lib.hgnn_graph_attention_workspace_bytes(i32(N), i32(G), i32(nh), i32(kv), i32(d), i32(nb), i32(dt), ctypes.byref(a), ctypes.byref(b))
+    assert size() == 0 and b.value >= 4 * 100 * 4 and size(dt=1) == 0 and b.value >= 4 * 100 * 4 + 4 * 100 * 4 * 32
+    for kw, code in ((dict(N=-1), SHAPE), (dict(G=-1), SHAPE), (dict(nh=0), SHAPE), (dict(nh=65, kv=1), SHAPE), (dict(kv=3), SHAPE), (dict(kv=0), SHAPE),
+                     (dict(kv=8), SHAPE), (dict(d=4), SHAPE), (dict(d=12), SHAPE), (dict(d=136), SHAPE), (dict(nb=0), SHAPE), (dict(nb=65), SHAPE),
+                     (dict(dt=2), SHAPE), (dict(N=1 << 28), OVERFLOW), (dict(N=200_000_000, G=100_000_000, nh=64, kv=1), OVERFLOW)):
+        assert size(**kw) == code, kw
+
+    def fwd(N=100, plan=P, pb=1 << 20, pairs=P, qkv=P, bias=P, out=P, saved=None, sb=0):
+        return lib.hgnn_graph_attention_fwd(None, i32(N), i32(3), i32(4), i32(2), i32(32), i32(8), i32(0), f32(1.0), plan, sz(pb), pairs, qkv, bias,
+                                            out, saved, sz(sb))
+    for kw, code in ((dict(plan=None), NULL), (dict(pairs=None), NULL), (dict(qkv=None), NULL), (dict(bias=None), NULL), (dict(out=None), NULL),
+                     (dict(pb=64), WS), (dict(saved=P, sb=64), WS), (dict(N=0, qkv=None), 0)):
+        assert fwd(**kw) == code, kw
+
+    def bwd(pb=1 << 20, saved=P, sb=1 << 20, g=P, gq=P, gb=P, ws=P, wb=1 << 20, out=P):
+        return lib.hgnn_graph_attention_bwd(None, i32(100), i32(3), i32(4), i32(2), i32(32), i32(8), i32(0), f32(1.0), P, sz(pb), P, P, P, out, saved,
+                                            sz(sb), g, gq, gb, ws, sz(wb))
+    for kw, code in ((dict(pb=64), WS), (dict(sb=64), WS), (dict(wb=64), WS), (dict(saved=None), NULL), (dict(g=None), NULL), (dict(gq=None), NULL),
+                     (dict(gb=None), NULL), (dict(ws=None), NULL), (dict(out=None), NULL)):
+        assert bwd(**kw) == code, kw
