@@ -509,13 +509,29 @@ __global__ void __launch_bounds__(256) k_attn_fwd(AttnArgs a) {
   }
 }
 
-// sum of this wavefront's columns of every bucket, and of the other wavefronts': out[b]
-__device__ __forceinline__ void hist_out(const float* hist, int nb, float* out, int lane) {
-  for (int b = lane; b < nb; b += 64) {
-    float s = 0.f;
-    for (int k = 0; k < 64; ++k) s += hist[b * 64 + ((k + lane) & 63)];
-    out[b] = s;
+// sum of a bucket's 64 columns (a lane per bucket: the columns are taken in turn, from its own on, so that no bank is hit twice)
+__device__ __forceinline__ float hist_sum(const float* hist, int b) {
+  float s[8] = {};
+#pragma unroll
+  for (int k = 0; k < 64; ++k) s[k & 7] += hist[b * 64 + ((k + b) & 63)];
+  return ((s[0] + s[4]) + (s[1] + s[5])) + ((s[2] + s[6]) + (s[3] + s[7]));
+}
+
+// adds x[k] to this lane's word at[k] of LDS, HB words at a time: they are read together, and one that is named twice takes up
+// what the earlier one has made of it. (Adding in LDS itself, ds_add_f32, took 210 cycles of the compute unit for 64 words.)
+constexpr int HB = 4;
+__device__ __forceinline__ void hist_add(float* hist, const unsigned (&at)[HB], const float (&x)[HB]) {
+  float v[HB];
+#pragma unroll
+  for (int k = 0; k < HB; ++k) v[k] = hist[at[k]];
+#pragma unroll
+  for (int k = 0; k < HB; ++k) {
+#pragma unroll
+    for (int u = 0; u < k; ++u) v[k] = at[k] == at[u] ? v[u] : v[k];
+    v[k] += x[k];
   }
+#pragma unroll
+  for (int k = 0; k < HB; ++k) hist[at[k]] = v[k];
 }
 
 // -------------------------------------------------------------------------------------------------------------------------
@@ -572,13 +588,21 @@ __global__ void __launch_bounds__(256) k_attn_dq(AttnArgs a) {
       lds_order();
       const u32x4_t bc = bk;
       if (j0 + step < w.n) fetch(j0 + step);
+      const bool real = qi < w.n;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const unsigned b = bucket_of(bc, i);
-        const float tb = table[b], p = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, tb) - lse);
-        ds[i] = p * (ds[i] - D);
-        const unsigned hb = tb > -__builtin_inff() ? b : (unsigned)a.nb;   // (one more column for what is left out)
-        __hip_atomic_fetch_add(&hist[hb * 64 + lane], qi < w.n ? ds[i] : 0.f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      for (int i0 = 0; i0 < 16; i0 += HB) {
+        unsigned at[HB];
+        float x[HB];
+#pragma unroll
+        for (int k = 0; k < HB; ++k) {
+          const int i = i0 + k;
+          const unsigned b = bucket_of(bc, i);
+          const float tb = table[b], p = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, tb) - lse);
+          ds[i] = p * (ds[i] - D);
+          at[k] = (real && tb > -__builtin_inff() ? b : (unsigned)a.nb) * 64 + lane;   // (a column for what is left out)
+          x[k] = ds[i];
+        }
+        hist_add(hist, at, x);
       }
       add_cols<BF, DP>(tk, Weights<BF>(ds), dq, lane);
     }
@@ -641,19 +665,15 @@ __global__ void __launch_bounds__(256) k_attn_dq(AttnArgs a) {
 
   lds_order();
   if (!a.split) {
-    if (me < a.per_head) hist_out(hist, a.nb, a.partial + ((size_t)h * a.per_head + me) * a.nb, lane);
+    if (me < a.per_head && lane < a.nb) a.partial[((size_t)h * a.per_head + me) * a.nb + lane] = hist_sum(hist, lane);
     return;
   }
   __syncthreads();
-  if (wave == 0) {
-    for (int b = lane; b < a.nb; b += 64) {
-      float s = 0.f;
-      for (int k2 = 0; k2 < a.nw; ++k2) {
-        const float* hw = reinterpret_cast<const float*>(smem + k2 * wave_bytes + 1024 + tile_bytes<BF, DP>());
-        for (int k = 0; k < 64; ++k) s += hw[b * 64 + ((k + lane) & 63)];
-      }
-      a.partial[((size_t)h * a.per_head + me) * a.nb + b] = s;
-    }
+  if (wave == 0 && lane < a.nb) {
+    float s = 0.f;
+    for (int k2 = 0; k2 < a.nw; ++k2)
+      s += hist_sum(reinterpret_cast<const float*>(smem + k2 * wave_bytes + 1024 + tile_bytes<BF, DP>()), lane);
+    a.partial[((size_t)h * a.per_head + me) * a.nb + lane] = s;
   }
 }
 
@@ -662,8 +682,16 @@ __device__ __forceinline__ void bias_reduce(const AttnArgs& a, int h, float* sh)
   const int b = threadIdx.x & 63, run = threadIdx.x >> 6, runs = blockDim.x >> 6;
   const int per = (a.per_head + runs - 1) / runs, k1 = min(a.per_head, (run + 1) * per);
   float s = 0.f;
-  if (b < a.nb)
-    for (int k = run * per; k < k1; ++k) s += a.partial[((size_t)h * a.per_head + k) * a.nb + b];
+  if (b < a.nb) {
+    const float* p = a.partial + (size_t)h * a.per_head * a.nb + b;
+    for (int k = run * per; k < k1; k += 16) {   // sixteen loads on their way at a time
+      float v[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) v[u] = k + u < k1 ? p[(size_t)(k + u) * a.nb] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 16; ++u) s += v[u];
+    }
+  }
   sh[threadIdx.x] = s;
   __syncthreads();
   if (run == 0 && b < a.nb) {
@@ -828,7 +856,7 @@ int waves_that_fit(int wave_bytes, int extra) {
 // wavefronts per head of the reverse kernel over queries: every tile its own while they are few, then as many as keep the chip
 // busy (each leaves one partial of g_bias)
 int64_t dq_per_head(int64_t max_tiles, int nh) {
-  const int64_t most = (8192 + nh - 1) / nh;
+  const int64_t most = (4096 + nh - 1) / nh;
   return max_tiles < most ? max_tiles : most;
 }
 
@@ -890,7 +918,7 @@ int32_t launch_bwd(hipStream_t st, AttnArgs a) {
   a.split = attn_split(a.plan.max_tiles, a.nh, a.G, a.N);
   {
     const int wb = dq_wave_bytes<BF, DP>(a.nb), extra = a.split ? join_bytes(DP) : 0;
-    a.nw = waves_that_fit(wb, extra);
+    a.nw = a.split ? waves_that_fit(wb, extra) : 1;   // (nothing is shared but in a split tile, and single wavefronts pack into LDS best)
     const int64_t groups = a.split ? a.per_head : (a.per_head + a.nw - 1) / a.nw;
     k_attn_dq<BF, DP><<<(unsigned)(groups * a.nh), 64 * a.nw, wb * a.nw + extra, st>>>(a);
     HGNN_LAUNCH_CHECK("k_attn_dq");
