@@ -55,6 +55,7 @@ enum { HGNN_F32 = 0, HGNN_BF16 = 1 };
 enum { HGNN_POOL_SUM = 0, HGNN_POOL_MEAN = 1 };
 enum { HGNN_NORM_RMS = 0, HGNN_NORM_LAYER = 1 };
 enum { HGNN_GATE_NONE = 0, HGNN_GATE_ATOM = 1, HGNN_GATE_CHANNEL = 2 };
+enum { HGNN_ACT_NONE = 0, HGNN_ACT_SILU = 1, HGNN_ACT_GELU = 2 };
 enum { HGNN_PAIR_NONE = 255 }; /* byte of a pair that is left out */
 enum { HGNN_ZMAX = 94 }; /* embedding table has HGNN_ZMAX+1 rows */
 
@@ -423,6 +424,26 @@ int32_t hgnn_graph_attention_bwd(void* stream, int32_t N, int32_t G, int32_t nh,
                                  float scale, const void* plan, size_t plan_bytes, const uint8_t* pairs,
                                  const void* qkv, const float* bias, const void* out, const void* saved, size_t saved_bytes,
                                  const void* g_out, void* g_qkv /*out*/, float* g_bias /*out*/, void* ws, size_t ws_bytes);
+
+/* ---------------------------------------------------------------------------------------------
+ * Dense product with bias, activation and residual in its epilogue, over M rows (atoms):
+ *   y = r + act(x W + b),  act: none, silu, or gelu z Phi(z) with the normal distribution's Phi (no approximation)
+ * x is T [M,K], W T [K,N] row-major, b float32 [N] or NULL, r T [M,N] or NULL, y T [M,N]; gW and g_b are float32. With dtype
+ * HGNN_F32 products are formed to float32 precision; with HGNN_BF16 x, W, r and y are bfloat16 in memory (hgnn_round_bf16 makes
+ * such a copy of a float32 weight buffer, nearest even) and y and g_x are rounded once, g_x from a g_z = g_y act'(z) that is
+ * rounded where it enters the product; gW and g_b carry no bf16 rounding.
+ * `saved` (NULL: no reverse pass follows) is written by _fwd and read by _bwd; it is empty without an activation.
+ * _bwd writes g_x (NULL: not wanted), gW and g_b (NULL: not wanted); the gradient of r is g_y itself. y may alias r.
+ * M >= 0, 1 <= K, N <= 8192 (else BAD_SHAPE); M <= 2^26 (else OVERFLOW). Only enqueue work.
+ * ------------------------------------------------------------------------------------------- */
+int32_t hgnn_dense_workspace_bytes(int32_t M, int32_t K, int32_t N, int32_t act, int32_t dtype, size_t* ws_bytes_host,
+                                   size_t* saved_bytes_host);
+int32_t hgnn_dense_fwd(void* stream, int32_t M, int32_t K, int32_t N, int32_t act, int32_t dtype, const void* x, const void* W,
+                       const float* b, const void* r, void* y /*out*/, void* saved /*or NULL*/, size_t saved_bytes);
+int32_t hgnn_dense_bwd(void* stream, int32_t M, int32_t K, int32_t N, int32_t act, int32_t dtype, const void* x, const void* W,
+                       const void* saved, size_t saved_bytes, const void* g_y, void* g_x /*out or NULL*/,
+                       float* gW /*out [K,N]*/, float* g_b /*out [N] or NULL*/, void* ws, size_t ws_bytes);
+int32_t hgnn_round_bf16(void* stream, int64_t n, const float* src, void* dst /*out, bf16*/);
 
 /* ---------------------------------------------------------------------------------------------
  * AdamW update of a flat float32 parameter buffer (paper, training setup: the optimiser is AdamW, learning rate 1e-3;

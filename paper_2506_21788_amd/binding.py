@@ -18,6 +18,7 @@ F32, BF16 = 0, 1
 POOL_SUM, POOL_MEAN = 0, 1
 NORM_RMS, NORM_LAYER = 0, 1
 GATE_NONE, GATE_ATOM, GATE_CHANNEL = 0, 1, 2
+ACT_NONE, ACT_SILU, ACT_GELU = 0, 1, 2
 PAIR_NONE = 255
 ZMAX = 94
 
@@ -35,6 +36,7 @@ EXPORTS = [
     "hgnn_block_norm_workspace_bytes", "hgnn_block_norm_fwd", "hgnn_block_norm_bwd",
     "hgnn_pair_plan_workspace_bytes", "hgnn_pair_plan", "hgnn_pair_buckets",
     "hgnn_graph_attention_workspace_bytes", "hgnn_graph_attention_fwd", "hgnn_graph_attention_bwd",
+    "hgnn_dense_workspace_bytes", "hgnn_dense_fwd", "hgnn_dense_bwd", "hgnn_round_bf16",
     "hgnn_adamw_step",
     "hgnn_profile_begin", "hgnn_profile_end", "hgnn_profile_num_tags", "hgnn_profile_tag_name",
     "hgnn_profile_read",
@@ -83,6 +85,7 @@ _deep_ws = _sig("hgnn_multihead_deep_workspace_bytes", i32, i32, i32, i32, i32, 
 _norm_ws = _sig("hgnn_block_norm_workspace_bytes", i32, i32, C.POINTER(sz), C.POINTER(sz))
 _pair_ws = _sig("hgnn_pair_plan_workspace_bytes", i32, i32, C.POINTER(sz))
 _attn_ws = _sig("hgnn_graph_attention_workspace_bytes", i32, i32, i32, i32, i32, i32, i32, C.POINTER(sz), C.POINTER(sz))
+_dense_ws = _sig("hgnn_dense_workspace_bytes", i32, i32, i32, i32, i32, C.POINTER(sz), C.POINTER(sz))
 
 
 def last_error_string() -> str:
@@ -304,6 +307,26 @@ def graph_attention_bwd(N, G, heads, kv_heads, head_dim, buckets, dtype, scale, 
                         g_bias, ws):
     _check(_n.graph_attention_bwd(N, G, heads, kv_heads, head_dim, buckets, dtype, scale, plan, pairs, qkv, bias, out, saved, g_out,
                                   g_qkv, g_bias, ws))
+
+
+def dense_workspace_bytes(M, K, N, act, dtype):
+    a, b = sz(0), sz(0)
+    _check(_dense_ws(M, K, N, act, dtype, C.byref(a), C.byref(b)))
+    return a.value, b.value
+
+
+def dense_fwd(M, K, N, act, dtype, x, W, b, r, y, saved):
+    _check(_n.dense_fwd(M, K, N, act, dtype, x, W, b, r, y, saved))
+
+
+def dense_bwd(M, K, N, act, dtype, x, W, saved, g_y, g_x, gW, g_b, ws):
+    _check(_n.dense_bwd(M, K, N, act, dtype, x, W, saved, g_y, g_x, gW, g_b, ws))
+
+
+def round_bf16(src, dst):
+    """dst (bfloat16) = src (float32), rounded to nearest even."""
+    assert src.numel() == dst.numel() and src.dtype == torch.float32 and dst.dtype == torch.bfloat16
+    _check(_n.round_bf16(src.numel(), src, dst))
 
 
 # ------------------------------------------------------------------------------------------------

@@ -1,0 +1,583 @@
+// hgnn_dense_fwd / _bwd: y = r + act(x W + b) and its gradients, x [M,K], W [K,N], and hgnn_round_bf16.
+//
+//   g_z = g_y act'(z),   g_x = g_z W^T,   gW = x^T g_z,   g_b = column sums of g_z
+//
+// Three products with operands in different orders, one kernel each way: a workgroup forms a tile of the result from slices
+// of 32 of the contraction that it stages in LDS as bf16 while the next slice is on its way from memory. An operand whose
+// neighbours in memory run along the contraction is staged row by row and read in 8-byte pieces, one whose neighbours run along
+// the result through transposing reads; both give a lane the contraction places 4 g + 0..3 and 8 + 4 g + 0..3 of 16.
+// float32 operands are staged as three bf16 terms and take six partial products (devmath.h): 2.7 times the rate of the float32
+// matrix cores at their precision. The forward pass keeps act'(z) in float32, so that the reverse pass multiplies by it where
+// it stages g_z: no tensor g_z exists. In gW, a sum over all rows, a bf16 call takes g_z as two bf16 terms, as the one
+// rounding that g_z = g_y act'(z) would suffer has no business in a float32 result.
+//
+// Small calls (few tiles) take k_dense_small: 32 x 32 results, the contraction dealt to the four wavefronts of a workgroup, operands
+// straight from memory: nothing is staged, the chain is one load, some products and a join.
+#include <climits>
+
+#include "common.h"
+#include "devmath.h"
+#include "prof.h"
+
+namespace hgnn {
+namespace {
+
+typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+
+struct Operand {
+  const void* p = nullptr;      // float32 or bf16
+  const float* mul = nullptr;   // float32 factors in the same places (act'), or null
+  int ld = 0;
+};
+
+struct DenseArgs {
+  int I, J, C;           // result I x J, contraction C
+  Operand a, b;          // a: [I][C] or [C][I], b: [J][C] or [C][J]
+  int act;
+  const float* bias;     // [J] or null
+  const void* res;       // [I][J] or null
+  void* out;             // [I][J]
+  float* dact;           // [I][J] act'(z) or null
+  float* partial;        // weight gradient: [nsplit][I][J], then colsum [nsplit][J]
+  float* colsum;         // [nsplit][J] column sums of b, or null
+  int nsplit, per_split; // contraction slices of a split (multiple of 32 places)
+  int ti, tj;            // tiles
+};
+
+// eight neighbouring values of an operand in float32; n of them exist (the others are zero)
+template <bool BF, bool MUL>
+__device__ __forceinline__ void load8(const Operand& o, size_t at, int n, float (&v)[8]) {
+  if (n >= 8) {
+    if constexpr (BF) {
+      u32x4_t w;
+      __builtin_memcpy(&w, static_cast<const unsigned short*>(o.p) + at, 16);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[2 * k] = __uint_as_float(w[k] << 16);
+        v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+      }
+    } else {
+      __builtin_memcpy(v, static_cast<const float*>(o.p) + at, 32);
+    }
+    if constexpr (MUL) {
+      float m[8];
+      __builtin_memcpy(m, o.mul + at, 32);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] *= m[k];
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      float x = 0.f;
+      if (k < n) {
+        if constexpr (BF) x = __uint_as_float((unsigned)static_cast<const unsigned short*>(o.p)[at + k] << 16);
+        else x = static_cast<const float*>(o.p)[at + k];
+        if constexpr (MUL) x *= o.mul[at + k];
+      }
+      v[k] = x;
+    }
+  }
+}
+
+// eight values as NT bf16 terms
+template <int NT>
+__device__ __forceinline__ void split8(const float (&x)[8], u32x4_t (&o)[NT]) {
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    if constexpr (NT == 3) {
+      unsigned p[3];
+      split_bf16x3_pair(x[2 * t], x[2 * t + 1], p);
+      o[0][t] = p[0]; o[1][t] = p[1]; o[2][t] = p[2];
+    } else {
+      const unsigned h = pack_bf16x2(x[2 * t], x[2 * t + 1]);
+      o[0][t] = h;
+      if constexpr (NT == 2) o[1][t] = pack_bf16x2(x[2 * t] - __uint_as_float(h << 16), x[2 * t + 1] - __uint_as_float(h & 0xffff0000u));
+    }
+  }
+}
+
+// acc += a b over the terms that count, smallest first
+template <int NA, int NB>
+__device__ __forceinline__ f32x16_t mfma_terms(const bf16x8_t (&a)[NA], const bf16x8_t (&b)[NB], f32x16_t acc) {
+  if constexpr (NA == 3 && NB == 3) return mfma_bf16x3(a, b, acc);
+  else {
+#pragma unroll
+    for (int t = NB - 1; t >= 0; --t) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b[t], acc, 0, 0, 0);
+    return acc;
+  }
+}
+
+__device__ __forceinline__ bf16x8_t cat(s16x4_t l, s16x4_t h) {
+  return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+constexpr int BC = 32;   // contraction places of a slice
+
+// A slice of an operand: E places along the result (E = 64 or 128) by BC along the contraction. KC: its neighbours in memory
+// run along the contraction. NT bf16 terms, one plane each.
+template <int E, bool KC, int NT>
+struct Slice {
+  static constexpr int PITCH = KC ? BC + 8 : E + 16;          // elements; rows of 16 bytes, in different groups of banks
+  static constexpr int PLANE = (KC ? E : BC) * PITCH;
+  static constexpr int BYTES = PLANE * NT * 2;
+  static constexpr int CH = E * BC / 8 / 256;                 // chunks of 8 of a thread
+  __device__ static __forceinline__ void place(int c, int& e, int& k) {   // of chunk c
+    if (KC) { e = c / (BC / 8); k = c % (BC / 8) * 8; }
+    else { k = c / (E / 8); e = c % (E / 8) * 8; }
+  }
+  template <bool BF, bool MUL>
+  __device__ static __forceinline__ void fetch(const Operand& o, int e0, int k0, int ne, int nk, int tid, float (&v)[CH][8]) {
+#pragma unroll
+    for (int u = 0; u < CH; ++u) {
+      int e, k;
+      place(tid + u * 256, e, k);
+      e += e0;
+      k += k0;
+      if (KC) load8<BF, MUL>(o, (size_t)(e < ne ? e : 0) * o.ld + (k < nk ? k : 0), e < ne ? nk - k : 0, v[u]);
+      else load8<BF, MUL>(o, (size_t)(k < nk ? k : 0) * o.ld + (e < ne ? e : 0), k < nk ? ne - e : 0, v[u]);
+    }
+  }
+  __device__ static __forceinline__ void stage(unsigned short* lds, int tid, const float (&v)[CH][8]) {
+#pragma unroll
+    for (int u = 0; u < CH; ++u) {
+      int e, k;
+      place(tid + u * 256, e, k);
+      u32x4_t t[NT];
+      split8<NT>(v[u], t);
+#pragma unroll
+      for (int q = 0; q < NT; ++q) *reinterpret_cast<u32x4_t*>(lds + q * PLANE + (KC ? e * PITCH + k : k * PITCH + e)) = t[q];
+    }
+  }
+  // operand of the 32 places from e on, contraction places 16 s + {4 g + 0..3, 8 + 4 g + 0..3}
+  __device__ static __forceinline__ void read(const unsigned short* lds, int e, int s, int lane, bf16x8_t (&o)[NT]) {
+#pragma unroll
+    for (int q = 0; q < NT; ++q) {
+      if constexpr (KC) {
+        const unsigned short* p = lds + q * PLANE + (e + (lane & 31)) * PITCH + 16 * s + 4 * (lane >> 5);
+        o[q] = cat(*reinterpret_cast<const s16x4_t*>(p), *reinterpret_cast<const s16x4_t*>(p + 8));
+      } else {
+        const unsigned short* p = lds + q * PLANE + (16 * s + 4 * (lane >> 5) + ((lane & 15) >> 2)) * PITCH + e + (lane & 16) + (lane & 3) * 4;
+        o[q] = cat(__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p)),
+                   __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p + 8 * PITCH)));
+      }
+    }
+  }
+};
+
+// act(z) and act'(z)
+__device__ __forceinline__ void activate(int act, float z, float& y, float& dy) {
+  if (act == HGNN_ACT_SILU) {
+    const float e = __expf(-fabsf(z)), r = 1.0f / (1.0f + e), s = z < 0.f ? e * r : r;   // (no overflow on either side)
+    y = z * s;
+    dy = s * (1.0f + z * (1.0f - s));
+  } else if (act == HGNN_ACT_GELU) {
+    const float phi = 0.5f * erfcf(-0.70710678118654752f * z);
+    y = z * phi;
+    dy = fmaf(0.39894228040143268f * z, __expf(-0.5f * z * z), phi);
+  } else {
+    y = z;
+    dy = 1.f;
+  }
+}
+
+enum { EPI_Y = 0, EPI_GX = 1, EPI_GW = 2 };
+
+// one value of the result
+template <bool BF, int EPI>
+__device__ __forceinline__ void finish(const DenseArgs& a, int i, int j, float v, int split) {
+  const size_t at = (size_t)i * a.J + j;
+  if constexpr (EPI == EPI_GW) {
+    a.partial[(size_t)split * a.I * a.J + at] = v;
+    return;
+  }
+  if constexpr (EPI == EPI_Y) {
+    if (a.bias) v += a.bias[j];
+    float y, dy;
+    activate(a.act, v, y, dy);
+    if (a.dact) a.dact[at] = dy;
+    v = y;
+    if (a.res) v += BF ? __uint_as_float((unsigned)static_cast<const unsigned short*>(a.res)[at] << 16) : static_cast<const float*>(a.res)[at];
+  }
+  if constexpr (BF) static_cast<unsigned short*>(a.out)[at] = (unsigned short)f2bf_bits(v);
+  else static_cast<float*>(a.out)[at] = v;
+}
+
+// tile of a workgroup: the tiles of a row block are neighbours on one XCD (workgroups are dealt to the 8 XCDs in turn), so its
+// rows come from memory once
+__device__ __forceinline__ bool tile_of(const DenseArgs& a, int& ti, int& tj, int& split) {
+  const int n = a.ti * a.tj * a.nsplit, per = (n + 7) / 8;
+  const int t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per || t >= n) return false;
+  tj = t % a.tj;
+  ti = t / a.tj % a.ti;
+  split = t / (a.tj * a.ti);
+  return true;
+}
+
+// EI x EJ tile, 2 x 2 wavefronts. AKC / BKC: the operand's neighbours run along the contraction.
+template <bool BF, int EPI, int EI, int EJ, bool AKC, bool BKC, int NA, int NB, bool AMUL, bool BMUL>
+__global__ void __launch_bounds__(256) k_dense(DenseArgs a) {
+  using SA = Slice<EI, AKC, NA>;
+  using SB = Slice<EJ, BKC, NB>;
+  extern __shared__ __align__(16) char smem[];
+  unsigned short* la = reinterpret_cast<unsigned short*>(smem);
+  unsigned short* lb = reinterpret_cast<unsigned short*>(smem + SA::BYTES);
+  constexpr int WI = EI / 64, WJ = EJ / 64;   // 32-blocks of a wavefront
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wi = wave >> 1, wj = wave & 1;
+  int ti, tj, split;
+  if (!tile_of(a, ti, tj, split)) return;
+  const int i0 = ti * EI, j0 = tj * EJ;
+  const int c0 = split * a.per_split, c1 = min(a.C, c0 + a.per_split);
+  f32x16_t acc[WI][WJ] = {};
+  float va[SA::CH][8], vb[SB::CH][8];
+  float cs[SB::CH][8] = {};
+  const bool sums = EPI == EPI_GW && a.colsum && ti == 0;
+  if (c0 < c1) {
+    SA::template fetch<BF, AMUL>(a.a, i0, c0, a.I, c1, tid, va);
+    SB::template fetch<BF, BMUL>(a.b, j0, c0, a.J, c1, tid, vb);
+  }
+  for (int c = c0; c < c1; c += BC) {
+    __syncthreads();
+    SA::stage(la, tid, va);
+    SB::stage(lb, tid, vb);
+    if (sums) {
+#pragma unroll
+      for (int u = 0; u < SB::CH; ++u)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) cs[u][k] += vb[u][k];
+    }
+    if (c + BC < c1) {
+      SA::template fetch<BF, AMUL>(a.a, i0, c + BC, a.I, c1, tid, va);
+      SB::template fetch<BF, BMUL>(a.b, j0, c + BC, a.J, c1, tid, vb);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < BC / 16; ++s) {
+      bf16x8_t fa[WI][NA], fb[WJ][NB];
+#pragma unroll
+      for (int i = 0; i < WI; ++i) SA::read(la, wi * (EI / 2) + i * 32, s, lane, fa[i]);
+#pragma unroll
+      for (int j = 0; j < WJ; ++j) SB::read(lb, wj * (EJ / 2) + j * 32, s, lane, fb[j]);
+#pragma unroll
+      for (int i = 0; i < WI; ++i)
+#pragma unroll
+        for (int j = 0; j < WJ; ++j) acc[i][j] = mfma_terms<NA, NB>(fa[i], fb[j], acc[i][j]);
+    }
+  }
+  if constexpr (EPI == EPI_GW) {
+    if (sums) {   // the threads that took the same columns, in order (a column's chunks: threads q, q + EJ/8, ...)
+      static_assert(!BKC, "the rows of the slice are contraction places");
+      __syncthreads();
+      float* sh = reinterpret_cast<float*>(smem);
+      constexpr int Q = EJ / 8;   // threads of a row; 256 / Q rows at a time
+#pragma unroll
+      for (int u = 1; u < SB::CH; ++u)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) cs[0][k] += cs[u][k];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sh[tid / Q * EJ + (tid % Q) * 8 + k] = cs[0][k];
+      __syncthreads();
+      if (tid < EJ && j0 + tid < a.J) {
+        float s = sh[tid];
+        for (int k = 1; k < 256 / Q; ++k) s += sh[k * EJ + tid];
+        a.colsum[(size_t)split * a.J + j0 + tid] = s;
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < WI; ++i)
+#pragma unroll
+    for (int j = 0; j < WJ; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int r = i0 + wi * (EI / 2) + i * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
+        const int q = j0 + wj * (EJ / 2) + j * 32 + (lane & 31);
+        if (r < a.I && q < a.J) finish<BF, EPI>(a, r, q, acc[i][j][v], split);
+      }
+}
+
+// 32 x 32 of the result; wavefront w takes contraction places 16 w + 64 t + 0..15
+template <bool BF, int EPI, bool AKC, bool BKC, int NA, int NB, bool AMUL, bool BMUL>
+__global__ void __launch_bounds__(256) k_dense_small(DenseArgs a) {
+  __shared__ float join[4][16][64];
+  __shared__ float cjoin[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
+  int ti, tj, split;
+  if (!tile_of(a, ti, tj, split)) return;
+  const int i = ti * 32 + (lane & 31), j = tj * 32 + (lane & 31);
+  const int c0 = split * a.per_split, c1 = min(a.C, c0 + a.per_split);
+  f32x16_t acc = {};
+  float cs = 0.f;
+  // the lane's eight contraction places c + 0..7 of row e of an operand
+  auto get = [&](auto kc, auto mul, const Operand& o, int e, int ne, int c, float (&v)[8]) {
+    if constexpr (decltype(kc)::value) {
+      load8<BF, decltype(mul)::value>(o, (size_t)(e < ne ? e : 0) * o.ld + (c < c1 ? c : 0), e < ne ? c1 - c : 0, v);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const bool ok = c + k < c1 && e < ne;
+        const size_t at = (size_t)(ok ? c + k : 0) * o.ld + (ok ? e : 0);
+        float x;
+        if constexpr (BF) x = __uint_as_float((unsigned)static_cast<const unsigned short*>(o.p)[at] << 16);
+        else x = static_cast<const float*>(o.p)[at];
+        if constexpr (decltype(mul)::value) x *= o.mul[at];
+        v[k] = ok ? x : 0.f;
+      }
+    }
+  };
+  for (int c = c0 + wave * 16; c < c1; c += 64) {
+    float x[8], y[8];
+    get(std::bool_constant<AKC>{}, std::bool_constant<AMUL>{}, a.a, i, a.I, c + 8 * g, x);
+    get(std::bool_constant<BKC>{}, std::bool_constant<BMUL>{}, a.b, j, a.J, c + 8 * g, y);
+    u32x4_t ua[NA], ub[NB];
+    split8<NA>(x, ua);
+    split8<NB>(y, ub);
+    bf16x8_t fa[NA], fb[NB];
+#pragma unroll
+    for (int q = 0; q < NA; ++q) fa[q] = __builtin_bit_cast(bf16x8_t, ua[q]);
+#pragma unroll
+    for (int q = 0; q < NB; ++q) fb[q] = __builtin_bit_cast(bf16x8_t, ub[q]);
+    acc = mfma_terms<NA, NB>(fa, fb, acc);
+    if constexpr (EPI == EPI_GW) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) cs += y[k];
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < 16; ++v) join[wave][v][lane] = acc[v];
+  if constexpr (EPI == EPI_GW) cjoin[wave][lane] = cs;
+  __syncthreads();
+  if constexpr (EPI == EPI_GW) {
+    if (wave == 0 && a.colsum && ti == 0 && lane < 32 && j < a.J) {
+      float s = 0.f;
+      for (int w = 0; w < 4; ++w) s += cjoin[w][lane] + cjoin[w][lane + 32];
+      a.colsum[(size_t)split * a.J + j] = s;
+    }
+  }
+  // the shares are added in the order of the wavefronts; each finishes four rows of every lane
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int v = 4 * wave + u;
+    const float s = ((join[0][v][lane] + join[1][v][lane]) + join[2][v][lane]) + join[3][v][lane];
+    const int r = ti * 32 + 8 * wave + 4 * g + u;
+    if (r < a.I && j < a.J) finish<BF, EPI>(a, r, j, s, split);
+  }
+}
+
+// gW and g_b: the splits' partials in order
+__global__ void __launch_bounds__(256) k_dense_reduce(const float* partial, const float* colsum, int nsplit, int64_t n, int J, float* gW, float* g_b) {
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const float* p;
+  int64_t stride;
+  float* out;
+  if (t < n) {
+    p = partial + t; stride = n; out = gW + t;
+  } else if (colsum && t - n < J) {
+    p = colsum + (t - n); stride = J; out = g_b + (t - n);
+  } else {
+    return;
+  }
+  float s = 0.f;
+  for (int k = 0; k < nsplit; k += 8) {
+    float v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = k + u < nsplit ? p[(k + u) * stride] : 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) s += v[u];
+  }
+  *out = s;
+}
+
+__global__ void k_dense_zero(float* gW, int64_t n, float* g_b, int J) {
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (t < n) gW[t] = 0.f;
+  if (g_b && t < J) g_b[t] = 0.f;
+}
+
+// float -> bf16, nearest even
+__global__ void __launch_bounds__(256) k_round_bf16(int64_t n, const float* src, unsigned short* dst) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (i + 8 <= n) {
+    const float4 x = *reinterpret_cast<const float4*>(src + i), y = *reinterpret_cast<const float4*>(src + i + 4);
+    const u32x4_t w = {pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w), pack_bf16x2(y.x, y.y), pack_bf16x2(y.z, y.w)};
+    *reinterpret_cast<u32x4_t*>(dst + i) = w;
+  } else {
+    for (int64_t k = i; k < n; ++k) dst[k] = (unsigned short)f2bf_bits(src[k]);
+  }
+}
+
+// -------------------------------------------------------------------------------------------------------------------------
+// Tiles of 128 fill the matrix cores best, but only with a workgroup for most compute units; below, tiles of 64, and where even
+// those would leave most of the chip idle, 32 x 32 with the contraction dealt out inside the workgroup.
+enum { SIZE_32, SIZE_64, SIZE_128 };
+int tile_size(int64_t I, int64_t J, int64_t splits) {
+  const int64_t cu = num_cus();
+  auto tiles = [&](int e) { return ((I + e - 1) / e) * ((J + e - 1) / e) * splits; };
+  if (tiles(128) >= cu) return SIZE_128;
+  return tiles(64) >= cu / 2 ? SIZE_64 : SIZE_32;
+}
+
+// Splits of the weight gradient's contraction (the rows): enough workgroups for two per compute unit, at least 128 rows each.
+struct WSplit {
+  int size, nsplit, per;
+};
+WSplit weight_split(int64_t M, int64_t K, int64_t N) {
+  const int64_t cu = num_cus();
+  for (int size : {SIZE_128, SIZE_64, SIZE_32}) {
+    const int e = size == SIZE_128 ? 128 : size == SIZE_64 ? 64 : 32;
+    const int64_t tiles = ((K + e - 1) / e) * ((N + e - 1) / e);
+    const int64_t want = (2 * cu + tiles - 1) / tiles, most = (M + 127) / 128;
+    int64_t s = want < most ? want : most;
+    if (s < 1) s = 1;
+    if (size != SIZE_32 && tiles * s < cu / 2) continue;   // a smaller tile makes more workgroups
+    int64_t per = (M + s - 1) / s;
+    per = (per + 63) / 64 * 64;
+    return {size, (int)((M + per - 1) / per), (int)per};
+  }
+  return {SIZE_32, 1, (int)M};
+}
+
+template <bool BF, int EPI, int E, bool AKC, bool BKC, int NA, int NB, bool AMUL, bool BMUL>
+int32_t launch_tile(hipStream_t st, const DenseArgs& a) {
+  const int lds_in = Slice<E, AKC, NA>::BYTES + Slice<E, BKC, NB>::BYTES, lds_cs = EPI == EPI_GW ? 256 * 8 * 4 : 0;
+  const int64_t n = (int64_t)a.ti * a.tj * a.nsplit;
+  k_dense<BF, EPI, E, E, AKC, BKC, NA, NB, AMUL, BMUL><<<(unsigned)((n + 7) / 8 * 8), 256, lds_in > lds_cs ? lds_in : lds_cs, st>>>(a);
+  HGNN_LAUNCH_CHECK("k_dense");
+  return HGNN_OK;
+}
+
+template <bool BF, int EPI, bool AKC, bool BKC, int NA, int NB, bool AMUL, bool BMUL>
+int32_t launch_size(hipStream_t st, DenseArgs a, int size) {
+  const int e = size == SIZE_128 ? 128 : size == SIZE_64 ? 64 : 32;
+  a.ti = (a.I + e - 1) / e;
+  a.tj = (a.J + e - 1) / e;
+  if (size == SIZE_128) return launch_tile<BF, EPI, 128, AKC, BKC, NA, NB, AMUL, BMUL>(st, a);
+  if (size == SIZE_64) return launch_tile<BF, EPI, 64, AKC, BKC, NA, NB, AMUL, BMUL>(st, a);
+  const int64_t n = (int64_t)a.ti * a.tj * a.nsplit;
+  k_dense_small<BF, EPI, AKC, BKC, NA, NB, AMUL, BMUL><<<(unsigned)((n + 7) / 8 * 8), 256, 0, st>>>(a);
+  HGNN_LAUNCH_CHECK("k_dense_small");
+  return HGNN_OK;
+}
+
+int32_t check_dense(int64_t M, int32_t K, int32_t N, int32_t act, int32_t dtype) {
+  HGNN_REQUIRE(M >= 0, HGNN_ERR_BAD_SHAPE, "negative number of rows");
+  HGNN_REQUIRE(K >= 1 && K <= 8192 && N >= 1 && N <= 8192, HGNN_ERR_BAD_SHAPE, "dense: widths must be in 1..8192 (got %d, %d)", K, N);
+  HGNN_REQUIRE(act == HGNN_ACT_NONE || act == HGNN_ACT_SILU || act == HGNN_ACT_GELU, HGNN_ERR_BAD_SHAPE, "unknown activation %d", act);
+  HGNN_REQUIRE(dtype == HGNN_F32 || dtype == HGNN_BF16, HGNN_ERR_BAD_SHAPE, "unknown dtype %d", dtype);
+  HGNN_REQUIRE(M <= (1 << 26), HGNN_ERR_OVERFLOW, "dense: at most 2^26 rows");
+  return HGNN_OK;
+}
+
+size_t saved_bytes_of(int64_t M, int N, int act) { return act == HGNN_ACT_NONE ? 0 : (size_t)M * N * sizeof(float); }
+size_t ws_bytes_of(int64_t M, int K, int N) {
+  if (M == 0) return 0;
+  const WSplit w = weight_split(M, K, N);
+  return w.nsplit > 1 ? (size_t)w.nsplit * ((size_t)K * N + N) * sizeof(float) : 0;
+}
+
+template <bool BF>
+int32_t run_fwd(hipStream_t st, const DenseArgs& a) {
+  return launch_size<BF, EPI_Y, true, false, BF ? 1 : 3, BF ? 1 : 3, false, false>(st, a, tile_size(a.I, a.J, 1));
+}
+
+template <bool BF, bool MUL>
+int32_t run_bwd(hipStream_t st, int M, int K, int N, const void* x, const void* W, const float* dact, const void* g_y, void* g_x, float* gW,
+                float* g_b, float* ws) {
+  if (g_x) {
+    DenseArgs a{};
+    a.I = M; a.J = K; a.C = N;
+    a.a = {g_y, dact, N};
+    a.b = {W, nullptr, N};
+    a.out = g_x; a.nsplit = 1; a.per_split = N;
+    HGNN_TRY((launch_size<BF, EPI_GX, true, true, BF ? 1 : 3, BF ? 1 : 3, MUL, false>(st, a, tile_size(M, K, 1))));
+  }
+  const WSplit w = weight_split(M, K, N);
+  DenseArgs a{};
+  a.I = K; a.J = N; a.C = M;
+  a.a = {x, nullptr, K};
+  a.b = {g_y, dact, N};
+  a.nsplit = w.nsplit; a.per_split = w.per;
+  const int64_t n = (int64_t)K * N;
+  a.partial = w.nsplit > 1 ? ws : gW;
+  a.colsum = g_b ? (w.nsplit > 1 ? ws + (size_t)w.nsplit * n : g_b) : nullptr;
+  HGNN_TRY((launch_size<BF, EPI_GW, false, false, BF ? 1 : 3, BF ? (MUL ? 2 : 1) : 3, false, MUL>(st, a, w.size)));
+  if (w.nsplit > 1) {
+    k_dense_reduce<<<(unsigned)((n + N + 255) / 256), 256, 0, st>>>(a.partial, a.colsum, w.nsplit, n, N, gW, g_b);
+    HGNN_LAUNCH_CHECK("k_dense_reduce");
+  }
+  return HGNN_OK;
+}
+
+}  // namespace
+}  // namespace hgnn
+
+using namespace hgnn;
+
+extern "C" int32_t hgnn_dense_workspace_bytes(int32_t M, int32_t K, int32_t N, int32_t act, int32_t dtype, size_t* ws_bytes_host,
+                                              size_t* saved_bytes_host) {
+  HGNN_TRY(check_dense(M, K, N, act, dtype));
+  HGNN_REQUIRE(ws_bytes_host && saved_bytes_host, HGNN_ERR_NULLPTR, "null size pointer");
+  *ws_bytes_host = ws_bytes_of(M, K, N);
+  *saved_bytes_host = saved_bytes_of(M, N, act);
+  return HGNN_OK;
+}
+
+extern "C" int32_t hgnn_dense_fwd(void* stream, int32_t M, int32_t K, int32_t N, int32_t act, int32_t dtype, const void* x, const void* W,
+                                  const float* b, const void* r, void* y, void* saved, size_t saved_bytes) {
+  HGNN_TRY(check_dense(M, K, N, act, dtype));
+  if (M == 0) return HGNN_OK;
+  HGNN_REQUIRE(x && W && y, HGNN_ERR_NULLPTR, "dense_fwd: null pointer");
+  const size_t need = saved_bytes_of(M, N, act);
+  HGNN_REQUIRE(!saved || saved_bytes >= need, HGNN_ERR_WORKSPACE_TOO_SMALL, "dense saved buffer: need %zu bytes, got %zu", need, saved_bytes);
+  DenseArgs a{};
+  a.I = M; a.J = N; a.C = K;
+  a.a = {x, nullptr, K};
+  a.b = {W, nullptr, N};
+  a.act = act; a.bias = b; a.res = r; a.out = y;
+  a.dact = act == HGNN_ACT_NONE ? nullptr : static_cast<float*>(saved);
+  a.nsplit = 1; a.per_split = K;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  ProfScope ps(PT_MISC, st);
+  return dtype == HGNN_BF16 ? run_fwd<true>(st, a) : run_fwd<false>(st, a);
+}
+
+extern "C" int32_t hgnn_dense_bwd(void* stream, int32_t M, int32_t K, int32_t N, int32_t act, int32_t dtype, const void* x, const void* W,
+                                  const void* saved, size_t saved_bytes, const void* g_y, void* g_x, float* gW, float* g_b, void* ws,
+                                  size_t ws_bytes) {
+  HGNN_TRY(check_dense(M, K, N, act, dtype));
+  HGNN_REQUIRE(gW, HGNN_ERR_NULLPTR, "dense_bwd: null pointer");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (M == 0) {
+    const int64_t n = (int64_t)K * N;
+    k_dense_zero<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(gW, n, g_b, N);
+    HGNN_LAUNCH_CHECK("k_dense_zero");
+    return HGNN_OK;
+  }
+  HGNN_REQUIRE(x && W && g_y, HGNN_ERR_NULLPTR, "dense_bwd: null pointer");
+  HGNN_REQUIRE(act == HGNN_ACT_NONE || saved, HGNN_ERR_NULLPTR, "dense_bwd: an activation needs the saved buffer");
+  const size_t need = saved_bytes_of(M, N, act), wneed = ws_bytes_of(M, K, N);
+  HGNN_REQUIRE(act == HGNN_ACT_NONE || saved_bytes >= need, HGNN_ERR_WORKSPACE_TOO_SMALL, "dense saved buffer: need %zu bytes, got %zu", need, saved_bytes);
+  HGNN_REQUIRE(wneed == 0 || ws, HGNN_ERR_NULLPTR, "dense_bwd: null workspace");
+  HGNN_REQUIRE(ws_bytes >= wneed, HGNN_ERR_WORKSPACE_TOO_SMALL, "dense workspace: need %zu bytes, got %zu", wneed, ws_bytes);
+  const float* d = static_cast<const float*>(saved);
+  float* w = static_cast<float*>(ws);
+  ProfScope ps(PT_MISC, st);
+  if (dtype == HGNN_BF16)
+    return act == HGNN_ACT_NONE ? run_bwd<true, false>(st, M, K, N, x, W, nullptr, g_y, g_x, gW, g_b, w)
+                                : run_bwd<true, true>(st, M, K, N, x, W, d, g_y, g_x, gW, g_b, w);
+  return act == HGNN_ACT_NONE ? run_bwd<false, false>(st, M, K, N, x, W, nullptr, g_y, g_x, gW, g_b, w)
+                              : run_bwd<false, true>(st, M, K, N, x, W, d, g_y, g_x, gW, g_b, w);
+}
+
+extern "C" int32_t hgnn_round_bf16(void* stream, int64_t n, const float* src, void* dst) {
+  HGNN_REQUIRE(n >= 0, HGNN_ERR_BAD_SHAPE, "negative count");
+  HGNN_REQUIRE(n < (int64_t)INT_MAX * 1024, HGNN_ERR_OVERFLOW, "round_bf16: too many values for one launch");
+  if (n == 0) return HGNN_OK;
+  HGNN_REQUIRE(src && dst, HGNN_ERR_NULLPTR, "round_bf16: null pointer");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  ProfScope ps(PT_MISC, st);
+  k_round_bf16<<<(unsigned)((n + 2047) / 2048), 256, 0, st>>>(n, src, static_cast<unsigned short*>(dst));
+  HGNN_LAUNCH_CHECK("k_round_bf16");
+  return HGNN_OK;
+}

@@ -136,6 +136,7 @@ PyMethodDef methods[] = {
     ENTRY(block_norm_fwd), ENTRY(block_norm_bwd),
     {"pair_plan", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call_pair_plan)), METH_FASTCALL, nullptr},
     ENTRY(pair_buckets), ENTRY(graph_attention_fwd), ENTRY(graph_attention_bwd),
+    ENTRY(dense_fwd), ENTRY(dense_bwd), ENTRY(round_bf16),
     ENTRY(adamw_step),
     {nullptr, nullptr, 0, nullptr},
 };

@@ -80,3 +80,27 @@ def test_graph_attention():
     for kw, code in ((dict(pb=64), WS), (dict(sb=64), WS), (dict(wb=64), WS), (dict(saved=None), NULL), (dict(g=None), NULL), (dict(gq=None), NULL),
                      (dict(gb=None), NULL), (dict(ws=None), NULL), (dict(out=None), NULL)):
         assert bwd(**kw) == code, kw
+
+
+def test_dense():
+    lib = _lib()
+    a, b = sz(0), sz(0)
+
+    def size(M=4000, K=64, N=96, act=1, dt=0):
+        return lib.hgnn_dense_workspace_bytes(i32(M), i32(K), i32(N), i32(act), i32(dt), ctypes.byref(a), ctypes.byref(b))
+    assert size() == 0 and b.value == 4000 * 96 * 4 and a.value > 0
+    assert size(act=0) == 0 and b.value == 0 and size(M=0) == 0 and a.value == 0
+    for kw, code in ((dict(M=-1), SHAPE), (dict(K=0), SHAPE), (dict(N=0), SHAPE), (dict(K=8193), SHAPE), (dict(N=8193), SHAPE), (dict(act=3), SHAPE),
+                     (dict(dt=2), SHAPE), (dict(M=(1 << 26) + 1), OVERFLOW)):
+        assert size(**kw) == code, kw
+    fwd = lambda x=P, W=P, y=P, s=None, sb=0, M=40: lib.hgnn_dense_fwd(None, i32(M), i32(64), i32(96), i32(1), i32(0), x, W, None, None, y, s, sz(sb))  # noqa: E731
+    for kw, code in ((dict(x=None), NULL), (dict(W=None), NULL), (dict(y=None), NULL), (dict(s=P, sb=8), WS), (dict(M=0, x=None), 0)):
+        assert fwd(**kw) == code, kw
+
+    def bwd(x=P, W=P, s=P, sb=1 << 30, g=P, gW=P, ws=P, wb=1 << 30, M=4000):
+        return lib.hgnn_dense_bwd(None, i32(M), i32(64), i32(96), i32(1), i32(0), x, W, s, sz(sb), g, P, gW, P, ws, sz(wb))
+    for kw, code in ((dict(x=None), NULL), (dict(W=None), NULL), (dict(s=None), NULL), (dict(g=None), NULL), (dict(gW=None), NULL), (dict(ws=None), NULL),
+                     (dict(wb=8), WS), (dict(sb=8), WS)):
+        assert bwd(**kw) == code, kw
+    assert lib.hgnn_round_bf16(None, i64(-1), P, P) == SHAPE and lib.hgnn_round_bf16(None, i64(4), None, P) == NULL
+    assert lib.hgnn_round_bf16(None, i64(1 << 42), P, P) == OVERFLOW and lib.hgnn_round_bf16(None, i64(0), None, None) == 0
