@@ -13,6 +13,7 @@ from .structures import (  # noqa: F401
 )
 from .configs import CONFIGS, make_config, small_mixed_batch  # noqa: F401
 from .weights import (  # noqa: F401
+    init_attention_weights,
     layer_weight_count,
     head_weight_count,
     LAYER_FIELDS,

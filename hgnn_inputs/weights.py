@@ -121,3 +121,19 @@ def upstream_grads(rng, G, N):
     """Seeded stand-in for dLoss/d(energy) [G] and dLoss/d(force) [N,3] (the loss is outside the path)."""
     return (rng.standard_normal(G).astype(np.float32),
             rng.standard_normal((N, 3)).astype(np.float32))
+
+
+def init_attention_weights(rng, H, fields, count):
+    """Flat parameter buffer of one global attention block; fields: name -> (first value, shape). Matrices as in the layers
+    (uniform, 1 / sqrt(inputs)), small biases, norms near 1 and a small residual scale."""
+    out = np.zeros(count, dtype=np.float32)
+    for name, (at, shape) in fields.items():
+        n = int(np.prod(shape))
+        if name in ("n1", "n2", "n3"):
+            v = rng.normal(0.0, 0.1, shape) + np.array([0.3, 1.0, 0.0, 1.0, 0.0])[:, None]
+        elif len(shape) == 2 and name != "bias":
+            v = rng.uniform(-1.0, 1.0, shape) * (3.0 / shape[0]) ** 0.5
+        else:
+            v = rng.normal(0.0, 0.1, shape)
+        out[at:at + n] = np.asarray(v, dtype=np.float32).reshape(-1)
+    return out

@@ -169,3 +169,43 @@ def dense_fwd(x, W, b, r, act):
 def dense_bwd(x, W, b, act, g_y):
     g = g_y * activation(x @ W + (0.0 if b is None else b), act)[1]
     return g @ W.T, x.T @ g, g.sum(0)
+
+
+# -- the whole block ----------------------------------------------------------------------------
+def unpack_block(flat, fields):
+    return {k: np.asarray(flat[a:a + int(np.prod(s))], np.float64).reshape(s) for k, (a, s) in fields.items()}
+
+
+def attention_block_fwd(h, W, pairs, graph_off, heads, kv_heads, layer, eps, act):
+    """h' and what the reverse pass needs; W: the block's parameters by name."""
+    N = h.shape[0]
+    d = W["Wo"].shape[0] // heads
+    c = dict(h=h, W=W, pairs=pairs, off=graph_off, heads=heads, kv=kv_heads, layer=layer, eps=eps, act=act, scale=d ** -0.5)
+    _, c["y1"] = block_norm_fwd(h, None, None, W["n1"], layer, eps)
+    c["qkv"] = dense_fwd(c["y1"], W["Wqkv"], W["bqkv"], None, "none").reshape(N, heads + 2 * kv_heads, d)
+    c["z"] = dense_fwd(c["y1"], W["Wg"], W["bg"], None, "none") if "Wg" in W else None
+    c["a"] = graph_attention(c["qkv"], W["bias"], pairs, graph_off, heads, kv_heads, c["scale"]).reshape(N, heads * d)
+    c["o"] = dense_fwd(c["a"], W["Wo"], W["bo"], None, "none")
+    c["h1"], c["y2"] = block_norm_fwd(h, c["o"], c["z"], W["n2"], layer, eps)
+    c["f"] = dense_fwd(c["y2"], W["W1"], W["b1"], None, act)
+    c["u"] = dense_fwd(c["f"], W["W2"], W["b2"], None, "none")
+    return block_norm_fwd(c["h1"], c["u"], None, W["n3"], layer, eps, False)[0], c
+
+
+def attention_block_bwd(c, g_out):
+    """Gradient with respect to h, and the parameters' by name."""
+    W, layer, eps, g = c["W"], c["layer"], c["eps"], {}
+    g_h1, g_u, _, g["n3"] = block_norm_bwd(c["h1"], c["u"], None, W["n3"], layer, eps, g_out, None)
+    g_f, g["W2"], g["b2"] = dense_bwd(c["f"], W["W2"], W["b2"], "none", g_u)
+    g_y2, g["W1"], g["b1"] = dense_bwd(c["y2"], W["W1"], W["b1"], c["act"], g_f)
+    g_h, g_o, g_z, g["n2"] = block_norm_bwd(c["h"], c["o"], c["z"], W["n2"], layer, eps, g_h1, g_y2)
+    g_a, g["Wo"], g["bo"] = dense_bwd(c["a"], W["Wo"], W["bo"], "none", g_o)
+    N = g_a.shape[0]
+    _, g_qkv, g["bias"] = graph_attention(c["qkv"], W["bias"], c["pairs"], c["off"], c["heads"], c["kv"], c["scale"],
+                                          g_a.reshape(N, c["heads"], -1))
+    g_y1, g["Wqkv"], g["bqkv"] = dense_bwd(c["y1"], W["Wqkv"], W["bqkv"], "none", g_qkv.reshape(N, -1))
+    if g_z is not None:
+        g_y, g["Wg"], g["bg"] = dense_bwd(c["y1"], W["Wg"], W["bg"], "none", g_z)
+        g_y1 = g_y1 + g_y
+    g_in, _, _, g["n1"] = block_norm_bwd(c["h"], None, None, W["n1"], layer, eps, g_h, g_y1)
+    return g_in, g

@@ -319,8 +319,8 @@ def dense_fwd(M, K, N, act, dtype, x, W, b, r, y, saved):
     _check(_n.dense_fwd(M, K, N, act, dtype, x, W, b, r, y, saved))
 
 
-def dense_bwd(M, K, N, act, dtype, x, W, saved, g_y, g_x, gW, g_b, ws):
-    _check(_n.dense_bwd(M, K, N, act, dtype, x, W, saved, g_y, g_x, gW, g_b, ws))
+def dense_bwd(M, K, N, act, dtype, x, W, saved, g_y, g_x, gW, g_b, ws, r_x=None):
+    _check(_n.dense_bwd(M, K, N, act, dtype, x, W, saved, g_y, r_x, g_x, gW, g_b, ws))
 
 
 def round_bf16(src, dst):

@@ -36,7 +36,7 @@ struct DenseArgs {
   Operand a, b;          // a: [I][C] or [C][I], b: [J][C] or [C][J]
   int act;
   const float* bias;     // [J] or null
-  const void* res;       // [I][J] or null
+  const void* res;       // [I][J] added to the result, or null
   void* out;             // [I][J]
   float* dact;           // [I][J] act'(z) or null
   float* partial;        // weight gradient: [nsplit][I][J], then colsum [nsplit][J]
@@ -197,6 +197,8 @@ __device__ __forceinline__ void finish(const DenseArgs& a, int i, int j, float v
     activate(a.act, v, y, dy);
     if (a.dact) a.dact[at] = dy;
     v = y;
+  }
+  if constexpr (EPI != EPI_GW) {
     if (a.res) v += BF ? __uint_as_float((unsigned)static_cast<const unsigned short*>(a.res)[at] << 16) : static_cast<const float*>(a.res)[at];
   }
   if constexpr (BF) static_cast<unsigned short*>(a.out)[at] = (unsigned short)f2bf_bits(v);
@@ -482,14 +484,14 @@ int32_t run_fwd(hipStream_t st, const DenseArgs& a) {
 }
 
 template <bool BF, bool MUL>
-int32_t run_bwd(hipStream_t st, int M, int K, int N, const void* x, const void* W, const float* dact, const void* g_y, void* g_x, float* gW,
-                float* g_b, float* ws) {
+int32_t run_bwd(hipStream_t st, int M, int K, int N, const void* x, const void* W, const float* dact, const void* g_y, const void* r_x,
+                void* g_x, float* gW, float* g_b, float* ws) {
   if (g_x) {
     DenseArgs a{};
     a.I = M; a.J = K; a.C = N;
     a.a = {g_y, dact, N};
     a.b = {W, nullptr, N};
-    a.out = g_x; a.nsplit = 1; a.per_split = N;
+    a.res = r_x; a.out = g_x; a.nsplit = 1; a.per_split = N;
     HGNN_TRY((launch_size<BF, EPI_GX, true, true, BF ? 1 : 3, BF ? 1 : 3, MUL, false>(st, a, tile_size(M, K, 1))));
   }
   const WSplit w = weight_split(M, K, N);
@@ -543,10 +545,10 @@ extern "C" int32_t hgnn_dense_fwd(void* stream, int32_t M, int32_t K, int32_t N,
 }
 
 extern "C" int32_t hgnn_dense_bwd(void* stream, int32_t M, int32_t K, int32_t N, int32_t act, int32_t dtype, const void* x, const void* W,
-                                  const void* saved, size_t saved_bytes, const void* g_y, void* g_x, float* gW, float* g_b, void* ws,
-                                  size_t ws_bytes) {
+                                  const void* saved, size_t saved_bytes, const void* g_y, const void* r_x, void* g_x, float* gW, float* g_b,
+                                  void* ws, size_t ws_bytes) {
   HGNN_TRY(check_dense(M, K, N, act, dtype));
-  HGNN_REQUIRE(gW, HGNN_ERR_NULLPTR, "dense_bwd: null pointer");
+  HGNN_REQUIRE(gW && (g_x || !r_x || M == 0), HGNN_ERR_NULLPTR, "dense_bwd: null pointer");
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (M == 0) {
     const int64_t n = (int64_t)K * N;
@@ -564,10 +566,10 @@ extern "C" int32_t hgnn_dense_bwd(void* stream, int32_t M, int32_t K, int32_t N,
   float* w = static_cast<float*>(ws);
   ProfScope ps(PT_MISC, st);
   if (dtype == HGNN_BF16)
-    return act == HGNN_ACT_NONE ? run_bwd<true, false>(st, M, K, N, x, W, nullptr, g_y, g_x, gW, g_b, w)
-                                : run_bwd<true, true>(st, M, K, N, x, W, d, g_y, g_x, gW, g_b, w);
-  return act == HGNN_ACT_NONE ? run_bwd<false, false>(st, M, K, N, x, W, nullptr, g_y, g_x, gW, g_b, w)
-                              : run_bwd<false, true>(st, M, K, N, x, W, d, g_y, g_x, gW, g_b, w);
+    return act == HGNN_ACT_NONE ? run_bwd<true, false>(st, M, K, N, x, W, nullptr, g_y, r_x, g_x, gW, g_b, w)
+                                : run_bwd<true, true>(st, M, K, N, x, W, d, g_y, r_x, g_x, gW, g_b, w);
+  return act == HGNN_ACT_NONE ? run_bwd<false, false>(st, M, K, N, x, W, nullptr, g_y, r_x, g_x, gW, g_b, w)
+                              : run_bwd<false, true>(st, M, K, N, x, W, d, g_y, r_x, g_x, gW, g_b, w);
 }
 
 extern "C" int32_t hgnn_round_bf16(void* stream, int64_t n, const float* src, void* dst) {

@@ -6,6 +6,7 @@ import numpy as np
 import torch
 
 from . import binding as B
+from .block import AttentionBlock, Pairs
 
 
 def _dev(a, dtype=None):
@@ -64,14 +65,17 @@ class HotPath:
     forward and backward. Inputs are numpy arrays (uploaded once); outputs stay on the device."""
 
     def __init__(self, batch, rc, H, L, S, dtype, emb, layer_weights, head_weights, alpha=None, Hh=None, D=None,
-                 rbf_k=None, move=False, pos_grad=False, keep_grads=False):
+                 rbf_k=None, move=False, pos_grad=False, keep_grads=False, attn=None, attn_weights=None):
         """D: hidden layers per head (the deep-head entry points); None: the one-hidden-layer heads.
         rbf_k: number of radial-basis edge attributes that take the place of d2 (None: d2 itself).
         move: the atoms move between layers (x = x0 + v): edge vectors, lengths and attributes are recomputed
         before every layer. pos_grad (implied by move): backward() also leaves the gradient with respect to the input
         positions in g_pos. Both run the layers through the edge-attribute entry points (bf16 operands).
         keep_grads: backward() keeps the gradient with respect to every layer's input (g_h[l], g_v[l], l = 0..L) instead
-        of ping-ponging between two buffers."""
+        of ping-ponging between two buffers.
+        attn: an AttentionConfig: every message-passing layer is followed by a global attention block over the atoms of each
+        structure, with the flat parameter buffers attn_weights[l]; backward() leaves their gradients in gWa[l]."""
+        self.attn = attn
         self.keep_grads = bool(keep_grads)
         self.move = bool(move)
         self.pos_grad = bool(pos_grad or move)
@@ -91,6 +95,9 @@ class HotPath:
         self.emb = _dev(emb, torch.float32)
         self.W = [_dev(w, torch.float32) for w in layer_weights]
         self.Whead = _dev(head_weights, torch.float32)
+        self.Wa = [_dev(w, torch.float32) for w in attn_weights] if attn else []
+        assert len(self.Wa) == (L if attn else 0), "one attention block per layer"
+        self.pairs = Pairs(attn, self.N, self.G) if attn else None
         self.alpha = alpha
         self.graph = Graph(self.pos, self.graph_off, self.cell, self.pbc, rc)
         self._alloc_E = None
@@ -103,7 +110,7 @@ class HotPath:
         b, hp = P["batch"], P["hp"]
         return cls(b, hp["rc"], hp["H"], hp["L"], hp["S"], hp["dtype"], P["emb"], P["Ws"], P["Wh"], alpha=alpha,
                    Hh=hp.get("Hh"), D=hp.get("D"), rbf_k=hp.get("rbf_k"), move=hp.get("move", False),
-                   pos_grad=hp.get("pos_grad", False), **kw)
+                   pos_grad=hp.get("pos_grad", False), attn=hp.get("attn"), attn_weights=P.get("Wa"), **kw)
 
     def build_plan(self):
         """Routing of graphs and atoms to their source's branch (depends on the batch only)."""
@@ -115,6 +122,8 @@ class HotPath:
         if self.alpha is None:
             self.alpha = 1.0 / max(1.0, self.graph.E / max(1, self.N))
         self._alloc(self.graph.E)
+        if self.attn:
+            self.pairs.build(self.pos, self.graph_off, self.cell, self.pbc)
         return self.graph
 
     def _alloc(self, E):
@@ -148,6 +157,13 @@ class HotPath:
         self.hsaved = _bytes(hsaved_b)
         self.h = [torch.empty((N, H), **f32) for _ in range(L + 1)]
         self.v = [torch.zeros((N, 3), **f32) for _ in range(L + 1)]   # v[0] stays zero: v^0 = 0
+        if self.attn:
+            self.blocks = []
+            for w in self.Wa:
+                self.blocks.append(AttentionBlock(self.attn, N, G, H, self.dtype, w, scratch=self.blocks[0] if self.blocks else None))
+            self.gWa = [b.gW for b in self.blocks]
+            self.h_mp = [torch.empty((N, H), **f32) for _ in range(L)]    # of the message passing, before the block
+            self.g_mp = torch.empty((N, H), **f32)
         self.p = torch.empty((G, H), **f32)
         self.energy = torch.empty(G, **f32)
         self.force = torch.empty((N, 3), **f32)
@@ -165,17 +181,20 @@ class HotPath:
         g, N, G, H = self.graph, self.N, self.G, self.H
         B.embed_fwd(N, H, self.Z, self.emb, self.h[0])
         for l in range(self.L):
+            h_out = self.h_mp[l] if self.attn else self.h[l + 1]
             if self.k is None:
                 B.mp_layer_fwd(N, g.E, H, self.dtype, self.alpha, g.row_ptr, g.dst, g.col, g.d2, g.rvec,
-                               self.h[l], self.v[l], self.W[l], self.h[l + 1], self.v[l + 1], self.saved[l], self.ws)
-                continue
-            if self.move:
-                B.edge_geometry_fwd(N, g.E, g.rvec, self.v[l], g.dst, g.col, self.rvec_l[l], self.d2_l[l])
-            if self.rbf_k is not None and (self.move or l == 0):
-                B.edge_rbf(g.E, self._d2(l), self.k, self.rc, self.attr_l[l])
-            B.mp_layer_attr_fwd(N, g.E, H, self.k, self.dtype, self.alpha, g.row_ptr, g.dst, g.col, self._attr(l),
-                                self._rvec(l), self.h[l], self.v[l], self.W[l], self.h[l + 1], self.v[l + 1],
-                                self.saved[l], self.ws)
+                               self.h[l], self.v[l], self.W[l], h_out, self.v[l + 1], self.saved[l], self.ws)
+            else:
+                if self.move:
+                    B.edge_geometry_fwd(N, g.E, g.rvec, self.v[l], g.dst, g.col, self.rvec_l[l], self.d2_l[l])
+                if self.rbf_k is not None and (self.move or l == 0):
+                    B.edge_rbf(g.E, self._d2(l), self.k, self.rc, self.attr_l[l])
+                B.mp_layer_attr_fwd(N, g.E, H, self.k, self.dtype, self.alpha, g.row_ptr, g.dst, g.col, self._attr(l),
+                                    self._rvec(l), self.h[l], self.v[l], self.W[l], h_out, self.v[l + 1],
+                                    self.saved[l], self.ws)
+            if self.attn:
+                self.blocks[l].forward(self.pairs, h_out, self.h[l + 1])
         B.pool_by_graph_fwd(N, G, H, B.POOL_MEAN, self.graph_off, self.h[-1], self.p)
         if self.D is None:
             B.multihead_decode_fwd(N, G, H, self.Hh, self.S, self.dtype, self.plan, self.p, self.h[-1], self.v[-1],
@@ -212,15 +231,19 @@ class HotPath:
         B.pool_by_graph_bwd(N, G, H, B.POOL_MEAN, self.graph_off, self.g_p, self.g_h[top], True)
         for l in reversed(range(self.L)):
             cur, nxt = at(l + 1), at(l)
+            g_h_mp = self.g_h[cur]
+            if self.attn:
+                g_h_mp = self.g_mp
+                self.blocks[l].backward(self.pairs, self.h_mp[l], self.h[l + 1], self.g_h[cur], g_h_mp)
             if self.k is None:
                 B.mp_layer_bwd(N, g.E, H, self.dtype, self.alpha, g.row_ptr, g.dst, g.col, g.d2, g.rvec, g.colT_ptr,
-                               g.permT, self.h[l], self.W[l], self.saved[l], self.g_h[cur], self.g_v[cur],
+                               g.permT, self.h[l], self.W[l], self.saved[l], g_h_mp, self.g_v[cur],
                                self.g_h[nxt], self.g_v[nxt], self.gW[l], self.ws)
             else:
                 pg = self.pos_grad
                 B.mp_layer_attr_bwd(N, g.E, H, self.k, self.dtype, self.alpha, g.row_ptr, g.dst, g.col, self._attr(l),
                                     self._rvec(l), g.colT_ptr, g.permT, self.h[l], self.W[l], self.saved[l],
-                                    self.g_h[cur], self.g_v[cur], self.g_h[nxt], self.g_v[nxt], self.gW[l],
+                                    g_h_mp, self.g_v[cur], self.g_h[nxt], self.g_v[nxt], self.gW[l],
                                     self.ws, g_attr=self.g_attr if pg else None, g_rvec=self.g_rvec if pg else None)
                 if pg:
                     if l == self.L - 1:

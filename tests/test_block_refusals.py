@@ -97,9 +97,9 @@ def test_dense():
     for kw, code in ((dict(x=None), NULL), (dict(W=None), NULL), (dict(y=None), NULL), (dict(s=P, sb=8), WS), (dict(M=0, x=None), 0)):
         assert fwd(**kw) == code, kw
 
-    def bwd(x=P, W=P, s=P, sb=1 << 30, g=P, gW=P, ws=P, wb=1 << 30, M=4000):
-        return lib.hgnn_dense_bwd(None, i32(M), i32(64), i32(96), i32(1), i32(0), x, W, s, sz(sb), g, P, gW, P, ws, sz(wb))
-    for kw, code in ((dict(x=None), NULL), (dict(W=None), NULL), (dict(s=None), NULL), (dict(g=None), NULL), (dict(gW=None), NULL), (dict(ws=None), NULL),
+    def bwd(x=P, W=P, s=P, sb=1 << 30, g=P, gx=P, gW=P, ws=P, wb=1 << 30, M=4000):
+        return lib.hgnn_dense_bwd(None, i32(M), i32(64), i32(96), i32(1), i32(0), x, W, s, sz(sb), g, P, gx, gW, P, ws, sz(wb))
+    for kw, code in ((dict(x=None), NULL), (dict(gx=None), NULL), (dict(W=None), NULL), (dict(s=None), NULL), (dict(g=None), NULL), (dict(gW=None), NULL), (dict(ws=None), NULL),
                      (dict(wb=8), WS), (dict(sb=8), WS)):
         assert bwd(**kw) == code, kw
     assert lib.hgnn_round_bf16(None, i64(-1), P, P) == SHAPE and lib.hgnn_round_bf16(None, i64(4), None, P) == NULL

@@ -26,7 +26,8 @@ def _case(M, K, N, act, dtype, bias=True, res=False, want_gx=True, seed=0, scale
     gW, g_b = empty((K, N)), empty(N) if bias else None
     B.dense_fwd(M, K, N, ACT[act], code, dx, dW, db, dev(r, dtype), y, saved)
     B.dense_fwd(M, K, N, ACT[act], code, dx, dW, db, dev(r, dtype), alone, None)
-    B.dense_bwd(M, K, N, ACT[act], code, dx, dW, saved, dg, g_x, gW, g_b, ws)
+    rx = rounded(rng.standard_normal((M, K)), dtype) if want_gx and res else None
+    B.dense_bwd(M, K, N, ACT[act], code, dx, dW, saved, dg, g_x, gW, g_b, ws, r_x=dev(rx, dtype))
     torch.cuda.synchronize()
     assert untouched(wg, sg) and torch.equal(y.view(torch.uint8), alone.view(torch.uint8))
 
@@ -43,7 +44,8 @@ def _case(M, K, N, act, dtype, bias=True, res=False, want_gx=True, seed=0, scale
     egz = np.abs(g) * (0.8 * ez + 16 * U32 * (1.0 + np.abs(z))) if act != "none" else np.zeros_like(gz)
     if want_gx:
         e = ((N + 8) * U32 * gz + egz + (UBF * gz if bf and act != "none" else 0.0)) @ np.abs(W).T
-        close("g_x", g_x, w_gx, e / U32, 1, dtype)
+        rx = 0.0 if rx is None else rx
+        close("g_x", g_x, w_gx + rx, e / U32 + np.abs(w_gx + rx), 1, dtype)
     # bf16: g_z enters gW as two terms, UBF^2 of it is lost
     e = np.abs(x).T @ ((M + 8) * U32 * gz + egz + (UBF ** 2 * gz if bf and act != "none" else 0.0))
     close("gW", gW, w_gW, e / U32, 1)

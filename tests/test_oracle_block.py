@@ -115,3 +115,22 @@ def test_dense_gradients_by_differences(act):
     for v, gv in zip((x, W, b), ob.dense_bwd(x, W, b, act, g)):
         at, d = _differences(loss, v, 15, rng)
         assert np.allclose(gv.reshape(-1)[at], d, rtol=1e-6, atol=1e-7)
+
+
+@pytest.mark.parametrize("gate", [None, "atom", "channel"])
+def test_block_gradients_by_differences(gate):
+    rng = np.random.default_rng(6)
+    off, H, nh, kv, d, F, nb = np.array([0, 3, 8]), 6, 2, 1, 4, 5, 3
+    shapes = {"n1": (5, H), "Wqkv": (H, (nh + 2 * kv) * d), "bqkv": ((nh + 2 * kv) * d,), "bias": (nh, nb), "Wo": (nh * d, H), "bo": (H,),
+              "n2": (5, H), "W1": (H, F), "b1": (F,), "W2": (F, H), "b2": (H,), "n3": (5, H)}
+    if gate:
+        shapes.update(Wg=(H, 1 if gate == "atom" else H), bg=(1 if gate == "atom" else H,))
+    W = {k: 0.5 * rng.standard_normal(s) for k, s in shapes.items()}
+    pairs = rng.integers(0, nb + 1, ob.pair_layout(off)[0][-1]).astype(np.uint8)
+    h, g = rng.standard_normal((8, H)), rng.standard_normal((8, H))
+    run = lambda: ob.attention_block_fwd(h, W, pairs, off, nh, kv, gate == "atom", 1e-5, "silu")  # noqa: E731
+    g_h, gW = ob.attention_block_bwd(run()[1], g)
+    loss = lambda: (run()[0] * g).sum()  # noqa: E731
+    for v, gv in [(h, g_h)] + [(W[k], gW[k]) for k in shapes]:
+        at, diff = _differences(loss, v, 12, rng)
+        assert np.allclose(gv.reshape(-1)[at], diff, rtol=1e-5, atol=1e-7)
