@@ -410,7 +410,7 @@ int32_t hgnn_pair_buckets(void* stream, int32_t N, int32_t G, const void* plan, 
  * Buckets have no gradient with respect to positions.
  * `saved` (NULL: no reverse pass follows) is written by _fwd and read by _bwd with the same out. plan: hgnn_pair_plan of this
  * batch; pairs: a pair matrix of it (its padding is not looked at).
- * 1 <= nh <= 64, nkv divides nh, dh a multiple of 8 in 8..128, 1 <= nb <= 64 (else BAD_SHAPE). N and G below 2^28, and
+ * 1 <= nh <= 64, nkv divides nh, dh a multiple of 8 in 8..128, 1 <= nb <= 64, 1e-6 <= scale <= 1e6 (else BAD_SHAPE). N and G below 2^28, and
  * (N / 32 + min(N, G) + 64) nh below 2^31 (else OVERFLOW). Only enqueue work.
  * dtype HGNN_BF16 rounds p and ds to bfloat16 where they enter the products of g_q, g_k and g_v; out, g_bias and all softmax
  * statistics are formed without such a rounding.

@@ -1,6 +1,6 @@
 // hgnn_graph_attention_fwd / _bwd: attention over the atoms of each graph with a learned bias per head and pair bucket.
 //
-//   s_ij = scale q_i . k_j + bias[h][bucket_ij],   p_ij = exp(s_ij - lse_i),   o_i = sum_j p_ij v_j
+//   s_ij = scale q_i . k_j + bias[h][bucket_ij],   p_ij = exp(s_ij - max) / sum,   o_i = sum_j p_ij v_j
 //   D_i = g_i . o_i,   ds_ij = p_ij (g_i . v_j - D_i),   g_q_i = scale sum_j ds_ij k_j,   g_k_j = scale sum_i ds_ij q_i,
 //   g_v_j = sum_i p_ij g_i,   g_bias[h][b] = sum of ds over the pairs of bucket b
 //
@@ -10,9 +10,13 @@
 // lane but for one exchange with the other half, the scale factors of a row are one register, and the packed weights are, as
 // they stand, the operand of the next product (O^T = V^T P^T, the order of its contraction being free). The rows of the first
 // operand are permuted (tile_row) so that the 16 keys of a lane are neighbours: their buckets are one 16-byte load. The bias
-// of a bucket is read from a table of 256 in LDS, which holds -inf past the last bucket, so a pair that is left out costs nothing.
+// of a bucket, in units of the product (bias / scale), is read from a table of 256 in LDS straight into the accumulators that the
+// product adds to; the table holds -inf past the last bucket, so a pair that is left out costs nothing.
 // Operands that a product needs by columns go through LDS once, row by row, and come back through transposing reads (bf16)
 // or as single values (float32, matrix-core products of float32).
+//
+// Bound by the vector units: a weight is an exponential (four issue slots) and some eight other operations, twice as many in
+// k_attn_dq, against 16 matrix-core cycles at a head width of 32.
 //
 // The sums of the reverse pass are split in two kernels (one owns queries, one keys) rather than added with atomics, so that
 // their order is fixed: the scores are formed twice. g_bias is collected in LDS, a column per lane and bucket (no two lanes
@@ -38,16 +42,15 @@ constexpr int ATTN_BUCKETS = 64;   // most buckets: a wavefront's sums of g_bias
 
 struct AttnArgs {
   int N, G, nh, nkv, dh, nb;
-  int nw;        // wavefronts of a workgroup
-  int split;     // 1: they share one tile of rows and deal the other side's tiles out, 0: a tile each
-  int per_head;  // wavefronts (split: workgroups) per head
-  float scale, c;   // c = scale log2 e
+  int nw;        // wavefronts of a workgroup: 1, or (SPLIT) those that share a tile of rows and deal out the other side's tiles
+  int per_head;  // workgroups per head of k_attn_dq
+  float scale, c, inv;   // c = scale log2 e, inv = 1 / scale
   PairPlan plan;
   const uint8_t* pairs;
   const void* qkv;
   const float* bias;
   void* out;
-  float* lse;     // [nh][N] log2 of the sum of exp, +inf for a row without pairs
+  float2* stat;   // [nh][N] largest score / scale, log2 of the sum of exp(score - largest); 0 and +inf for a row without pairs
   float* o32;     // [N][nh][dh] the output before its rounding (bf16), else null
   const void* g_out;
   void* g_qkv;
@@ -63,13 +66,20 @@ __device__ __forceinline__ void lds_order() { __builtin_amdgcn_fence(__ATOMIC_AC
 
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
 
+// 16-byte piece `piece` of row `row` of a bf16 tile in LDS. Rows are a multiple of 64 bytes long and 64 or 192 bytes apart (mod 256), so that a
+// transposing read (four rows of 64 bytes at a time) meets every bank once; within each 64 bytes the pieces are exchanged by
+// the row's place, so that sixteen rows read at one piece (in either order of rows) do too.
+__device__ __forceinline__ int piece_at(int row, int piece, int pitch) {
+  return row * pitch + ((piece ^ ((row >> 2) & 3) ^ ((row >> 4) * 2)) * 8);
+}
+
 // One row of DP (dh and zeros) per lane pair, as the operand of a product that contracts over it.
 // bf16: dims 16 k + 8 g + 0..7 of step k. float32: dims g DP/2 + s of step s.
 template <bool BF, int DP>
 struct Row;
 template <int DP>
 struct Row<true, DP> {
-  static constexpr int PITCH = DP + 16;   // elements of a row in LDS: rows 0..3 in four different groups of banks
+  static constexpr int PITCH = DP == 32 ? 32 : DP + 32;   // elements from row to row in LDS
   using T = unsigned short;
   u32x4_t f[DP / 16];
   __device__ __forceinline__ void load(const T* p, int dh, int g) {
@@ -80,12 +90,11 @@ struct Row<true, DP> {
       if (d < dh) f[k] = *reinterpret_cast<const u32x4_t*>(p + d);
     }
   }
-  __device__ __forceinline__ void to_lds(T* row, int g) const {
+  __device__ __forceinline__ void from_lds(const T* tile, int row, int g) {
 #pragma unroll
-    for (int k = 0; k < DP / 16; ++k) *reinterpret_cast<u32x4_t*>(row + 16 * k + 8 * g) = f[k];
+    for (int k = 0; k < DP / 16; ++k) f[k] = *reinterpret_cast<const u32x4_t*>(tile + piece_at(row, 2 * k + g, PITCH));
   }
-  __device__ __forceinline__ static f32x16_t dot(const Row& a, const Row& b) {
-    f32x16_t acc = {};
+  __device__ __forceinline__ static f32x16_t dot(const Row& a, const Row& b, f32x16_t acc) {
 #pragma unroll
     for (int k = 0; k < DP / 16; ++k)
       acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a.f[k]), __builtin_bit_cast(bf16x8_t, b.f[k]), acc, 0, 0, 0);
@@ -122,13 +131,14 @@ struct Row<false, DP> {
       f[4 * k] = v.x; f[4 * k + 1] = v.y; f[4 * k + 2] = v.z; f[4 * k + 3] = v.w;
     }
   }
-  __device__ __forceinline__ void to_lds(T* row, int g) const {
+  __device__ __forceinline__ void from_lds(const T* tile, int row, int g) {
 #pragma unroll
-    for (int k = 0; k < DP / 8; ++k)
-      *reinterpret_cast<float4*>(row + g * (DP / 2) + 4 * k) = make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
+    for (int k = 0; k < DP / 8; ++k) {
+      const float4 v = *reinterpret_cast<const float4*>(tile + row * PITCH + g * (DP / 2) + 4 * k);
+      f[4 * k] = v.x; f[4 * k + 1] = v.y; f[4 * k + 2] = v.z; f[4 * k + 3] = v.w;
+    }
   }
-  __device__ __forceinline__ static f32x16_t dot(const Row& a, const Row& b) {
-    f32x16_t acc = {};
+  __device__ __forceinline__ static f32x16_t dot(const Row& a, const Row& b, f32x16_t acc) {
 #pragma unroll
     for (int s = 0; s < DP / 2; ++s) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.f[s], b.f[s], acc, 0, 0, 0);
     return acc;
@@ -147,15 +157,46 @@ struct Row<false, DP> {
   }
 };
 
+// 32 rows on their way from memory to LDS, in pieces of 16 bytes: neighbouring lanes hold neighbouring pieces of a row. (Loaded as
+// operands, a lane its own row, every lane's piece was an access of its own to the cache: 320 a tile and wavefront, the
+// vector cache 64 % busy with looking them up; so it is a quarter of that.)
+template <bool BF, int DP>
+struct Tile {
+  using T = typename Row<BF, DP>::T;
+  static constexpr int EP = 16 / sizeof(T), NP = DP / EP;   // elements of a piece, pieces of a row
+  u32x4_t f[NP / 2];
+  // p: the tile's first row (uniform); rows: how many exist (the last one stands for those behind it)
+  __device__ __forceinline__ void load(const T* p, unsigned ld, int rows, int dh, int lane) {
+#pragma unroll
+    for (int u = 0; u < NP / 2; ++u) {
+      const int row = (u * 64 + lane) / NP, d = (u * 64 + lane) % NP * EP;
+      f[u] = u32x4_t{0, 0, 0, 0};
+      if (d < dh) f[u] = *reinterpret_cast<const u32x4_t*>(p + (unsigned)(min(row, rows - 1) * ld + d));
+    }
+  }
+  __device__ __forceinline__ void to_lds(T* tile, int lane) const {
+#pragma unroll
+    for (int u = 0; u < NP / 2; ++u) {
+      const int row = (u * 64 + lane) / NP, piece = (u * 64 + lane) % NP;
+      T* at;
+      if constexpr (BF) at = tile + piece_at(row, piece, Row<BF, DP>::PITCH);
+      else at = tile + row * Row<BF, DP>::PITCH + piece * EP;
+      *reinterpret_cast<u32x4_t*>(at) = f[u];
+    }
+  }
+};
+
 __device__ __forceinline__ bf16x8_t read_tr(const unsigned short* lo, const unsigned short* hi) {
   const s16x4_t l = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(lo));
   const s16x4_t h = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(hi));
   return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7));
 }
-// rows 16 g + 8 t + 0..7 of column col0 + lane & 31 of a tile in LDS
-__device__ __forceinline__ bf16x8_t read_col(const unsigned short* tile, int pitch, int col0, int t, int lane) {
-  const unsigned short* p = tile + (16 * (lane >> 5) + 8 * t + ((lane & 15) >> 2)) * pitch + col0 + (lane & 16) + (lane & 3) * 4;
-  return read_tr(p, p + 4 * pitch);
+// rows 16 g + 8 t + 0..7 of column 32 b + lane & 31 of a tile in LDS
+__device__ __forceinline__ bf16x8_t read_col(const unsigned short* tile, int pitch, int b, int t, int lane) {
+  const int row = 16 * (lane >> 5) + 8 * t + ((lane & 15) >> 2);   // (row / 4 is 2 t mod 4, and 2 t + 1 for the rows behind)
+  const int piece = (((lane >> 4) & 1) * 2 + ((lane >> 1) & 1)) ^ ((lane >> 5) * 2), within = (lane & 1) * 4;
+  const unsigned short* p = tile + row * pitch + 32 * b + within;
+  return read_tr(p + (piece ^ (2 * t & 3)) * 8, p + 4 * pitch + (piece ^ ((2 * t + 1) & 3)) * 8);
 }
 
 // sixteen weights of a lane's query (rows 16 g + v), packed as the second operand of a product over those rows
@@ -202,7 +243,7 @@ __device__ __forceinline__ void add_cols(const typename Row<BF, DP>::T* tile, co
     if constexpr (BF) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
-        acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_col(tile, PITCH, 32 * b, t, lane), w.w[t], acc[b], 0, 0, 0);
+        acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_col(tile, PITCH, b, t, lane), w.w[t], acc[b], 0, 0, 0);
     } else {
 #pragma unroll
       for (int v = 0; v < 16; ++v)
@@ -217,7 +258,7 @@ __device__ __forceinline__ void add_cols2(const unsigned short* tile, const Weig
   for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const bf16x8_t c = read_col(tile, Row<true, DP>::PITCH, 32 * b, t, lane);
+      const bf16x8_t c = read_col(tile, Row<true, DP>::PITCH, b, t, lane);
       acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c, w2.w[t], acc[b], 0, 0, 0);
       acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c, w.w[t], acc[b], 0, 0, 0);
     }
@@ -232,7 +273,7 @@ __device__ __forceinline__ void add_cols_lds(const typename Row<BF, DP>::T* tile
       const bf16x8_t o = read_col(w, WP, 0, t, lane);
 #pragma unroll
       for (int b = 0; b < DP / 32; ++b)
-        acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_col(tile, PITCH, 32 * b, t, lane), o, acc[b], 0, 0, 0);
+        acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_col(tile, PITCH, b, t, lane), o, acc[b], 0, 0, 0);
     }
   } else {
 #pragma unroll
@@ -248,46 +289,80 @@ __device__ __forceinline__ void add_cols_lds(const typename Row<BF, DP>::T* tile
 // a lane's sixteen weights as row lane & 31 of a tile in LDS, columns 16 g + 0..15
 template <bool BF>
 __device__ __forceinline__ void weights_to_lds(const Weights<BF>& w, typename Row<BF, 32>::T* tile, int lane) {
-  typename Row<BF, 32>::T* p = tile + (lane & 31) * Row<BF, 32>::PITCH + 16 * (lane >> 5);
   if constexpr (BF) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) *reinterpret_cast<u32x4_t*>(p + 8 * t) = __builtin_bit_cast(u32x4_t, w.w[t]);
+    for (int t = 0; t < 2; ++t)
+      *reinterpret_cast<u32x4_t*>(tile + piece_at(lane & 31, 2 * (lane >> 5) + t, Row<BF, 32>::PITCH)) = __builtin_bit_cast(u32x4_t, w.w[t]);
   } else {
+    typename Row<BF, 32>::T* p = tile + (lane & 31) * Row<BF, 32>::PITCH + 16 * (lane >> 5);
 #pragma unroll
     for (int t = 0; t < 4; ++t) *reinterpret_cast<float4*>(p + 4 * t) = make_float4(w.w[4 * t], w.w[4 * t + 1], w.w[4 * t + 2], w.w[4 * t + 3]);
   }
 }
 
-// byte v of a lane's sixteen buckets
-__device__ __forceinline__ unsigned bucket_of(const u32x4_t& w, int v) { return (w[v >> 2] >> (8 * (v & 3))) & 255u; }
+// byte v of a lane's sixteen buckets, shifted left by SH: the place of its entry in a table of 4- or 8-byte entries (one instruction)
+template <int SH>
+__device__ __forceinline__ unsigned entry_of(const u32x4_t& w, int v) {
+  const unsigned x = w[v >> 2], sh = SH;
+  unsigned r;
+  switch (v & 3) {
+    case 0: asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(r) : "v"(sh), "v"(x)); break;
+    case 1: asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(r) : "v"(sh), "v"(x)); break;
+    case 2: asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(r) : "v"(sh), "v"(x)); break;
+    default: asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3" : "=v"(r) : "v"(sh), "v"(x)); break;
+  }
+  return r;
+}
+// LDS by its address (the kernels have no LDS but the dynamic one, which begins at 0)
+template <class V>
+using Lds = __attribute__((address_space(3))) V;
+typedef float f32x2v_t __attribute__((ext_vector_type(2)));
+template <class V>
+__device__ __forceinline__ Lds<V>& lds(unsigned at) { return *(Lds<V>*)(uintptr_t)at; }
 
 // the buckets of the keys j0 + 16 g + 0..15 of a row; those past the graph's last atom become HGNN_PAIR_NONE
-__device__ __forceinline__ u32x4_t load_buckets(const uint8_t* row, int j0, int n, int g) {
-  const int j = j0 + 16 * g;
-  u32x4_t w = *reinterpret_cast<const u32x4_t*>(row + j);
+__device__ __forceinline__ u32x4_t load_buckets(const uint8_t* at, int j0, int n, int g) {
+  u32x4_t w = *reinterpret_cast<const u32x4_t*>(at);
   if (j0 + 32 > n) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const int left = n - (j + 4 * k);   // valid bytes of this word
+      const int left = n - (j0 + 16 * g + 4 * k);   // valid bytes of this word
       if (left < 4) w[k] |= left <= 0 ? 0xffffffffu : 0xffffffffu << (8 * left);
     }
   }
   return w;
 }
 
-// bias table of one head in units of log2 e: 256 entries, -inf for what is no bucket (a wavefront fills its own). A bias of the
-// lowest finite value stays finite: such a row is still a softmax over its pairs.
-__device__ __forceinline__ void fill_table(float* table, const float* bias, int nb, int lane) {
+// a bias in units of the product, -inf for what is no bucket. A finite one stays finite: a row of the lowest values is still a
+// softmax over its pairs.
+__device__ __forceinline__ float table_value(const float* bias, int nb, int b, float inv) {
+  if (b >= nb) return -__builtin_inff();
+  const float x = bias[b], v = x * inv;
+  return fabsf(x) < __builtin_inff() ? fminf(fmaxf(v, -3.4028235e38f), 3.4028235e38f) : v;
+}
+// 256 of them, by one wavefront
+__device__ __forceinline__ void fill_table(float* table, const float* bias, int nb, float inv, int lane) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int b = k * 64 + lane;
-    float v = -__builtin_inff();
-    if (b < nb) {
-      const float x = bias[b];
-      v = x * LOG2E;
-      if (fabsf(x) < __builtin_inff()) v = fminf(fmaxf(v, -3.4028235e38f), 3.4028235e38f);
-    }
-    table[b] = v;
+  for (int k = 0; k < 4; ++k) table[k * 64 + lane] = table_value(bias, nb, k * 64 + lane, inv);
+}
+__device__ __forceinline__ f32x16_t biases(unsigned table, const u32x4_t& w) {
+  f32x16_t t;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) t[i] = lds<const float>(entry_of<2>(w, i) + table);
+  return t;
+}
+
+// weights of sixteen scores (in units of the product): 2^(c (s - m) - l). Where every c m is small the exponent is one multiply-add;
+// a large one would lose its low places there (a bias of -1e9 as a mask), and s - m comes first.
+__device__ __forceinline__ void weights_of(f32x16_t& s, float c, float m, float l) {
+  const float cm = c * m;
+  if (__all(fabsf(cm) <= 64.f)) {
+    const float e = -cm - l;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, e));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i] - m, c, -l));
   }
 }
 
@@ -329,88 +404,109 @@ __device__ __forceinline__ bool all_finite(const f32x16_t (&acc)[NB], float more
   return __all(!counts || z == 0.f);
 }
 
-// where a wavefront's rows are
+// where a workgroup's rows are (t: uniform)
 struct Where {
-  int g, lo, n, i0;        // graph, its first atom, its atoms, first row of the tile
+  int lo, n, i0;           // the graph's first atom, its atoms, first row of the tile
   int64_t pitch;
   const uint8_t* pairs;    // the graph's matrix
 };
 __device__ __forceinline__ Where tile_where(const AttnArgs& a, int t) {
+  const PairTile r = a.plan.tile[t];
   Where w;
-  w.g = __builtin_amdgcn_readfirstlane(a.plan.tile_graph[t]);
-  w.lo = __builtin_amdgcn_readfirstlane(a.plan.graph_off[w.g]);
-  w.n = __builtin_amdgcn_readfirstlane(a.plan.graph_off[w.g + 1]) - w.lo;
-  w.i0 = (t - __builtin_amdgcn_readfirstlane(a.plan.tile_off[w.g])) * PAIR_T;
-  w.pitch = pair_pitch(w.n);
-  w.pairs = a.pairs + a.plan.pair_off[w.g];
+  w.lo = r.lo;
+  w.n = r.n;
+  w.i0 = r.i0;
+  w.pitch = pair_pitch(r.n);
+  w.pairs = a.pairs + r.off;
   return w;
 }
 
-// bytes of LDS of one wavefront (tables first)
+// LDS: the tables first, then each wavefront's tiles, then (SPLIT) room for the join
 template <bool BF, int DP>
 constexpr int tile_bytes() { return 32 * Row<BF, DP>::PITCH * (BF ? 2 : 4); }
-template <bool BF, int DP>
-constexpr int fwd_wave_bytes() { return 1024 + tile_bytes<BF, DP>(); }
-template <bool BF, int DP>
-int dq_wave_bytes(int nb) { return 1024 + tile_bytes<BF, DP>() + (nb + 1) * 256; }
-template <bool BF, int DP>
-constexpr int dkv_wave_bytes() { return 1024 + 2 * tile_bytes<BF, DP>() + 2 * tile_bytes<BF, 32>(); }
 constexpr int join_bytes(int DP) { return DP * 32 * 4 + 512; }
+constexpr int FWD_TABLE = 1024, DQ_TABLE = 2048;   // entries of 4 bytes; of 8: bias and place in the sums of g_bias
+template <bool BF, int DP>
+__host__ __device__ constexpr int dq_wave_bytes(int nb) { return 2 * tile_bytes<BF, DP>() + (nb + 1) * 256; }
+template <bool BF, int DP>
+constexpr int dkv_wave_bytes() { return 2 * tile_bytes<BF, DP>() + 2 * tile_bytes<BF, 32>(); }
+
+// x of the wavefronts of a workgroup, added in order: the sum is wavefront 0's
+template <int NB>
+__device__ __forceinline__ void join_sum(f32x16_t (&x)[NB], float* room, int nw, int wave, int lane) {
+  for (int k = 1; k < nw; ++k) {
+    __syncthreads();
+    if (wave == k) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) room[(b * 16 + i) * 64 + lane] = x[b][i];
+    }
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[b][i] += room[(b * 16 + i) * 64 + lane];
+    }
+  }
+}
 
 // -------------------------------------------------------------------------------------------------------------------------
-template <bool BF, int DP>
-__global__ void __launch_bounds__(256) k_attn_fwd(AttnArgs a) {
+template <bool BF, int DP, bool SPLIT>
+__global__ void __launch_bounds__(256, DP == 128 ? 1 : 2) k_attn_fwd(AttnArgs a) {
   using T = typename Row<BF, DP>::T;
   extern __shared__ __align__(16) char smem[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
-  const int group = blockIdx.x / a.nh, h = blockIdx.x - group * a.nh;
-  const int t = a.split ? group : group * a.nw + wave;
-  if (t >= a.plan.tile_off[a.G]) return;   // split: uniform over the workgroup
+  const int lane = threadIdx.x & 63, wave = SPLIT ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0, g = lane >> 5;
+  const int t = blockIdx.x / a.nh, h = blockIdx.x - t * a.nh;
+  if (t >= *a.plan.count) return;   // uniform over the workgroup
   const Where w = tile_where(a, t);
-  char* mine = smem + wave * fwd_wave_bytes<BF, DP>();
-  float* table = reinterpret_cast<float*>(mine);
-  T* tv = reinterpret_cast<T*>(mine + 1024);
-  fill_table(table, a.bias + (size_t)h * a.nb, a.nb, lane);
+  float* table = reinterpret_cast<float*>(smem);
+  T* tk = reinterpret_cast<T*>(smem + FWD_TABLE + wave * 2 * tile_bytes<BF, DP>());
+  T* tv = tk + 32 * Row<BF, DP>::PITCH;
+  fill_table(table, a.bias + (size_t)h * a.nb, a.nb, a.inv, lane);   // (SPLIT: the same values by every wavefront)
+  lds_order();
 
   const int hk = h / (a.nh / a.nkv);
-  const size_t ld = (size_t)(a.nh + 2 * a.nkv) * a.dh;   // elements of an atom's q, k, v
+  const unsigned ld = (unsigned)(a.nh + 2 * a.nkv) * a.dh;   // elements of an atom's q, k, v
   const T* base = static_cast<const T*>(a.qkv) + (size_t)w.lo * ld;
-  const int qi = w.i0 + (lane & 31), qc = qi < w.n ? qi : w.n - 1;
-  Row<BF, DP> q, k, v;
-  q.load(base + qc * ld + (size_t)h * a.dh, a.dh, g);
+  const int qi = w.i0 + (lane & 31), ql = min(lane & 31, w.n - 1 - w.i0);
+  Row<BF, DP> q, k;
+  q.load(base + (size_t)w.i0 * ld + (size_t)h * a.dh + ql * ld, a.dh, g);
   const T* kbase = base + (size_t)(a.nh + hk) * a.dh;
   const T* vbase = kbase + (size_t)a.nkv * a.dh;
-  const uint8_t* prow = w.pairs + qc * w.pitch;
+  const uint8_t* prow = w.pairs + w.i0 * w.pitch;
+  const unsigned pl = (unsigned)ql * (unsigned)w.pitch + 16 * g;
+  Tile<BF, DP> kt, vt;
   u32x4_t bk;
-  auto fetch = [&](int j0) {
-    const int jk = j0 + tile_row(lane & 31), jv = j0 + (lane & 31);
-    k.load(kbase + (size_t)(jk < w.n ? jk : w.n - 1) * ld, a.dh, g);
-    v.load(vbase + (size_t)(jv < w.n ? jv : w.n - 1) * ld, a.dh, g);
-    bk = load_buckets(prow, j0, w.n, g);
+  auto fetch = [&](int j0) {   // (addresses: a uniform one and a lane's offset within the tile)
+    kt.load(kbase + (size_t)j0 * ld, ld, w.n - j0, a.dh, lane);
+    vt.load(vbase + (size_t)j0 * ld, ld, w.n - j0, a.dh, lane);
+    bk = load_buckets(prow + j0 + pl, j0, w.n, g);
   };
 
-  float m = -__builtin_inff(), l = 0.f;
+  float m = -__builtin_inff(), l = 0.f;   // m in units of the product
   f32x16_t o[DP / 32] = {};
-  const int step = a.split ? a.nw * PAIR_T : PAIR_T;
-  int j0 = a.split ? wave * PAIR_T : 0;
+  const int step = SPLIT ? a.nw * PAIR_T : PAIR_T;
+  const float slack = 8.f / a.c;
+  int j0 = wave * PAIR_T;
   if (j0 < w.n) fetch(j0);
   for (; j0 < w.n; j0 += step) {
-    f32x16_t s = Row<BF, DP>::dot(k, q);
     lds_order();
-    v.to_lds(tv + (lane & 31) * Row<BF, DP>::PITCH, g);
+    kt.to_lds(tk, lane);
+    vt.to_lds(tv, lane);
+    f32x16_t s = biases(0, bk);
     lds_order();
-    const u32x4_t bc = bk;
     if (j0 + step < w.n) fetch(j0 + step);
-    float top = -__builtin_inff();
+    k.from_lds(tk, tile_row(lane & 31), g);
+    s = Row<BF, DP>::dot(k, q, s);
+    float top = s[0];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      s[i] = fmaf(s[i], a.c, table[bucket_of(bc, i)]);
-      top = fmaxf(top, s[i]);
-    }
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
     top = fmaxf(top, other_half(top));
     // the sums are rescaled only where a maximum has grown by 2^8: weights up to that size lose nothing
-    if (__any(top > m + 8.f || (m == -__builtin_inff() && top > m))) {
-      const float mn = fmaxf(m, top), f = mn == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+    if (__any(top > m + slack || (m == -__builtin_inff() && top > m))) {
+      const float mn = fmaxf(m, top), f = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m - mn) * a.c);
       m = mn;
       l *= f;
 #pragma unroll
@@ -418,22 +514,21 @@ __global__ void __launch_bounds__(256) k_attn_fwd(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[b][i] *= f;
     }
-    const float mu = m == -__builtin_inff() ? 0.f : m;
+    weights_of(s, a.c, m == -__builtin_inff() ? 0.f : m, 0.f);
+    float l4[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      s[i] = __builtin_amdgcn_exp2f(s[i] - mu);
-      l += s[i];
-    }
+    for (int i = 4; i < 16; ++i) l4[i & 3] += s[i];
+    l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
     const Weights<BF> p(s);
     // bf16: the weights enter as two terms. The reverse pass takes D from the output, and one rounding of the weights (2^-9) there
-    // is more than the bias gradient, a sum of differences, can bear; two more products and 40 operations of some 180 a tile
+    // is more than the bias gradient, a sum of differences, can bear; two more products and 40 operations of some 200 a tile
     if constexpr (BF) add_cols2<DP>(tv, p, remainder_of(s, p), o, lane);
     else add_cols<BF, DP>(tv, p, o, lane);
   }
   l += other_half(l);
 
-  if (a.split) {   // the wavefronts' shares, in order
-    char* join = smem + a.nw * fwd_wave_bytes<BF, DP>();
+  if constexpr (SPLIT) {   // the wavefronts' shares, in order
+    char* join = smem + FWD_TABLE + a.nw * 2 * tile_bytes<BF, DP>();
     float* jo = reinterpret_cast<float*>(join);
     float* jm = reinterpret_cast<float*>(join + DP * 32 * 4);
     for (int k2 = 1; k2 < a.nw; ++k2) {
@@ -446,11 +541,10 @@ __global__ void __launch_bounds__(256) k_attn_fwd(AttnArgs a) {
         if (lane < 32) { jm[lane] = m; jm[32 + lane] = l; }
       }
       __syncthreads();
-      if (wave == 0) {
-        const float m2 = jm[lane & 31], l2 = jm[32 + (lane & 31)];
-        const float mn = fmaxf(m, m2);
-        const float f1 = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - mn), f2 = m2 == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m2 - mn);
-        // (a sum that is no number stays one)
+      if (wave == 0) {   // (a sum that is no number stays one)
+        const float m2 = jm[lane & 31], l2 = jm[32 + (lane & 31)], mn = fmaxf(m, m2);
+        const float f1 = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m - mn) * a.c);
+        const float f2 = m2 == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m2 - mn) * a.c);
         l = l * f1 + l2 * f2;
         m = mn;
 #pragma unroll
@@ -476,7 +570,7 @@ __global__ void __launch_bounds__(256) k_attn_fwd(AttnArgs a) {
             if (BF && a.o32) store4<false>(a.o32, orow * a.dh + d, o[b], r, f);
           }
         }
-      if (a.lse && g == 0) a.lse[(size_t)h * a.N + w.lo + qi] = l > 0.f ? m + __log2f(l) : __builtin_inff();
+      if (a.stat && g == 0) a.stat[(size_t)h * a.N + w.lo + qi] = l > 0.f ? make_float2(m, __log2f(l)) : make_float2(0.f, __builtin_inff());
     }
     return;
   }
@@ -493,9 +587,9 @@ __global__ void __launch_bounds__(256) k_attn_fwd(AttnArgs a) {
       const size_t kj = ((size_t)w.lo + j) * ld + (size_t)(a.nh + hk) * a.dh, vj = kj + (size_t)a.nkv * a.dh;
       const float k0 = d0 ? value<BF>(a.qkv, kj + lane) : 0.f, k1 = d1 ? value<BF>(a.qkv, kj + lane + 64) : 0.f;
       const float v0 = d0 ? value<BF>(a.qkv, vj + lane) : 0.f, v1 = d1 ? value<BF>(a.qkv, vj + lane + 64) : 0.f;
-      const float s = fmaf(wave_sum(fmaf(q0, k0, q1 * k1)), a.c, b);
+      const float s = wave_sum(fmaf(q0, k0, q1 * k1)) + b;
       if (s == -__builtin_inff()) continue;
-      const float mn = fmaxf(mr, s), f = mr == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(mr - mn), p = __builtin_amdgcn_exp2f(s - mn);
+      const float mn = fmaxf(mr, s), f = mr == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((mr - mn) * a.c), p = __builtin_amdgcn_exp2f((s - mn) * a.c);
       mr = mn;
       lr = lr * f + p;
       o0 = o0 * f + p * v0;
@@ -505,7 +599,7 @@ __global__ void __launch_bounds__(256) k_attn_fwd(AttnArgs a) {
     const float f = lr == 0.f ? 0.f : 1.0f / lr;
     if (d0) { put<BF>(a.out, out + lane, o0 * f); if (BF && a.o32) a.o32[out + lane] = o0 * f; }
     if (d1) { put<BF>(a.out, out + lane + 64, o1 * f); if (BF && a.o32) a.o32[out + lane + 64] = o1 * f; }
-    if (a.lse && lane == 0) a.lse[(size_t)h * a.N + w.lo + w.i0 + r] = lr == 0.f ? __builtin_inff() : mr + __log2f(lr);
+    if (a.stat && lane == 0) a.stat[(size_t)h * a.N + w.lo + w.i0 + r] = lr == 0.f ? make_float2(0.f, __builtin_inff()) : make_float2(mr, __log2f(lr));
   }
 }
 
@@ -517,13 +611,13 @@ __device__ __forceinline__ float hist_sum(const float* hist, int b) {
   return ((s[0] + s[4]) + (s[1] + s[5])) + ((s[2] + s[6]) + (s[3] + s[7]));
 }
 
-// adds x[k] to this lane's word at[k] of LDS, HB words at a time: they are read together, and one that is named twice takes up
-// what the earlier one has made of it. (Adding in LDS itself, ds_add_f32, took 210 cycles of the compute unit for 64 words.)
+// adds x[k] to this lane's word at LDS address at[k], HB words at a time: they are read together, and one that is named twice
+// takes up what the earlier one has made of it. (Adding in LDS itself, ds_add_f32, took 210 cycles of the compute unit for 64 words.)
 constexpr int HB = 4;
-__device__ __forceinline__ void hist_add(float* hist, const unsigned (&at)[HB], const float (&x)[HB]) {
+__device__ __forceinline__ void hist_add(const unsigned (&at)[HB], const float (&x)[HB]) {
   float v[HB];
 #pragma unroll
-  for (int k = 0; k < HB; ++k) v[k] = hist[at[k]];
+  for (int k = 0; k < HB; ++k) v[k] = lds<float>(at[k]);
 #pragma unroll
   for (int k = 0; k < HB; ++k) {
 #pragma unroll
@@ -531,104 +625,105 @@ __device__ __forceinline__ void hist_add(float* hist, const unsigned (&at)[HB], 
     v[k] += x[k];
   }
 #pragma unroll
-  for (int k = 0; k < HB; ++k) hist[at[k]] = v[k];
+  for (int k = 0; k < HB; ++k) lds<float>(at[k]) = v[k];
 }
 
 // -------------------------------------------------------------------------------------------------------------------------
-// g_q of 32 queries, D of theirs, and g_bias. A wavefront (split: a workgroup) of head h takes tiles w, w + per_head, ...
-template <bool BF, int DP>
-__global__ void __launch_bounds__(256) k_attn_dq(AttnArgs a) {
+// g_q of 32 queries, D of theirs, and g_bias. A workgroup of head h takes tiles me, me + per_head, ...
+template <bool BF, int DP, bool SPLIT>
+__global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k_attn_dq(AttnArgs a) {
   using T = typename Row<BF, DP>::T;
   extern __shared__ __align__(16) char smem[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
-  const int group = blockIdx.x / a.nh, h = blockIdx.x - group * a.nh;
-  const int me = a.split ? group : group * a.nw + wave;
-  const int wave_bytes = 1024 + tile_bytes<BF, DP>() + (a.nb + 1) * 256;
-  char* mine = smem + wave * wave_bytes;
-  float* table = reinterpret_cast<float*>(mine);
-  T* tk = reinterpret_cast<T*>(mine + 1024);
-  float* hist = reinterpret_cast<float*>(mine + 1024 + tile_bytes<BF, DP>());
-  fill_table(table, a.bias + (size_t)h * a.nb, a.nb, lane);
+  const int lane = threadIdx.x & 63, wave = SPLIT ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0, g = lane >> 5;
+  const int me = blockIdx.x / a.nh, h = blockIdx.x - me * a.nh;
+  const int wave_bytes = dq_wave_bytes<BF, DP>(a.nb);
+  float2* table = reinterpret_cast<float2*>(smem);
+  T* tk = reinterpret_cast<T*>(smem + DQ_TABLE + wave * wave_bytes);
+  T* tv = tk + 32 * Row<BF, DP>::PITCH;
+  const unsigned hist_at = DQ_TABLE + wave * wave_bytes + 2 * tile_bytes<BF, DP>();
+  float* hist = reinterpret_cast<float*>(smem + hist_at);
+  // a bucket's bias and the place of its column; what is left out, by its byte or a bias of -inf, has a column of its own
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float v = table_value(a.bias + (size_t)h * a.nb, a.nb, k * 64 + lane, a.inv);
+    table[k * 64 + lane] = make_float2(v, __uint_as_float((v > -__builtin_inff() ? k * 64 + lane : a.nb) * 256u));
+  }
   for (int b = 0; b <= a.nb; ++b) hist[b * 64 + lane] = 0.f;
+  lds_order();
+  const unsigned my_col = hist_at + lane * 4;
   const int hk = h / (a.nh / a.nkv);
-  const size_t ld = (size_t)(a.nh + 2 * a.nkv) * a.dh, lo_ = (size_t)a.nh * a.dh;
-  const int ntiles = a.plan.tile_off[a.G];
+  const unsigned ld = (unsigned)(a.nh + 2 * a.nkv) * a.dh, lo_ = (unsigned)a.nh * a.dh;
+  const int ntiles = *a.plan.count;
 
-  for (int t = me < a.per_head ? me : ntiles; t < ntiles; t += a.per_head) {   // split: uniform over the workgroup
+  for (int t = me; t < ntiles; t += a.per_head) {   // uniform over the workgroup
     const Where w = tile_where(a, t);
     const T* base = static_cast<const T*>(a.qkv) + (size_t)w.lo * ld;
-    const int qi = w.i0 + (lane & 31), qc = qi < w.n ? qi : w.n - 1;
+    const int qi = w.i0 + (lane & 31), ql = min(lane & 31, w.n - 1 - w.i0);
+    const bool real = qi < w.n;
     Row<BF, DP> q, go, k, v;
-    q.load(base + qc * ld + (size_t)h * a.dh, a.dh, g);
-    go.load(static_cast<const T*>(a.g_out) + ((size_t)w.lo + qc) * lo_ + (size_t)h * a.dh, a.dh, g);
-    const float* o32 = BF ? a.o32 : static_cast<const float*>(a.out);
-    float D = go.dot32(o32 + ((size_t)w.lo + qc) * lo_ + (size_t)h * a.dh, a.dh, g);
+    q.load(base + (size_t)w.i0 * ld + (size_t)h * a.dh + ql * ld, a.dh, g);
+    const size_t orow = ((size_t)w.lo + w.i0) * lo_ + (size_t)h * a.dh;
+    go.load(static_cast<const T*>(a.g_out) + orow + ql * lo_, a.dh, g);
+    float D = go.dot32((BF ? a.o32 : static_cast<const float*>(a.out)) + orow + ql * lo_, a.dh, g);
     D += other_half(D);
-    const float lse = qi < w.n ? a.lse[(size_t)h * a.N + w.lo + qi] : __builtin_inff();
-    if (qi < w.n && g == 0 && (!a.split || wave == 0)) a.delta[(size_t)h * a.N + w.lo + qi] = D;
+    const float2 st = real ? a.stat[(size_t)h * a.N + w.lo + qi] : make_float2(0.f, __builtin_inff());
+    if (real && g == 0 && wave == 0) a.delta[(size_t)h * a.N + w.lo + qi] = D;
     const T* kbase = base + (size_t)(a.nh + hk) * a.dh;
+    const uint8_t* prow = w.pairs + w.i0 * w.pitch;
     const T* vbase = kbase + (size_t)a.nkv * a.dh;
-    const uint8_t* prow = w.pairs + qc * w.pitch;
+    const unsigned pl = (unsigned)ql * (unsigned)w.pitch + 16 * g;
+    const unsigned none = real ? 0u : 0xffffffffu;   // a row past the last atom: no pairs
+    Tile<BF, DP> kt, vt;
     u32x4_t bk;
     auto fetch = [&](int j0) {
-      const int j = j0 + tile_row(lane & 31);
-      const size_t r = (size_t)(j < w.n ? j : w.n - 1) * ld;
-      k.load(kbase + r, a.dh, g);
-      v.load(vbase + r, a.dh, g);
-      bk = load_buckets(prow, j0, w.n, g);
+      kt.load(kbase + (size_t)j0 * ld, ld, w.n - j0, a.dh, lane);
+      vt.load(vbase + (size_t)j0 * ld, ld, w.n - j0, a.dh, lane);
+      bk = load_buckets(prow + j0 + pl, j0, w.n, g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) bk[i] |= none;
     };
     f32x16_t dq[DP / 32] = {};
-    const int step = a.split ? a.nw * PAIR_T : PAIR_T;
-    int j0 = a.split ? wave * PAIR_T : 0;
+    const int step = SPLIT ? a.nw * PAIR_T : PAIR_T;
+    int j0 = wave * PAIR_T;
     if (j0 < w.n) fetch(j0);
     for (; j0 < w.n; j0 += step) {
-      f32x16_t s = Row<BF, DP>::dot(k, q), ds = Row<BF, DP>::dot(v, go);
       lds_order();
-      k.to_lds(tk + tile_row(lane & 31) * Row<BF, DP>::PITCH, g);
-      lds_order();
-      const u32x4_t bc = bk;
-      if (j0 + step < w.n) fetch(j0 + step);
-      const bool real = qi < w.n;
+      kt.to_lds(tk, lane);
+      vt.to_lds(tv, lane);
+      f32x16_t s;
+      unsigned at[16];
 #pragma unroll
-      for (int i0 = 0; i0 < 16; i0 += HB) {
-        unsigned at[HB];
+      for (int i = 0; i < 16; ++i) {
+        const f32x2v_t e = lds<const f32x2v_t>(entry_of<3>(bk, i));
+        s[i] = e[0];
+        at[i] = __float_as_uint(e[1]) + my_col;
+      }
+      lds_order();
+      if (j0 + step < w.n) fetch(j0 + step);
+      k.from_lds(tk, tile_row(lane & 31), g);
+      s = Row<BF, DP>::dot(k, q, s);
+      v.from_lds(tv, tile_row(lane & 31), g);
+      f32x16_t ds = Row<BF, DP>::dot(v, go, f32x16_t{});
+      weights_of(s, a.c, st.x, st.y);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) ds[i] = s[i] * (ds[i] - D);
+      add_cols<BF, DP>(tk, Weights<BF>(ds), dq, lane);
+#pragma unroll
+      for (int i = 0; i < 16; i += HB) {
+        unsigned ha[HB];
         float x[HB];
 #pragma unroll
-        for (int k = 0; k < HB; ++k) {
-          const int i = i0 + k;
-          const unsigned b = bucket_of(bc, i);
-          const float tb = table[b], p = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, tb) - lse);
-          ds[i] = p * (ds[i] - D);
-          at[k] = (real && tb > -__builtin_inff() ? b : (unsigned)a.nb) * 64 + lane;   // (a column for what is left out)
-          x[k] = ds[i];
-        }
-        hist_add(hist, at, x);
+        for (int u = 0; u < HB; ++u) { ha[u] = at[i + u]; x[u] = ds[i + u]; }
+        hist_add(ha, x);
       }
-      add_cols<BF, DP>(tk, Weights<BF>(ds), dq, lane);
     }
-    if (a.split) {
-      float* jo = reinterpret_cast<float*>(smem + a.nw * wave_bytes);
-      for (int k2 = 1; k2 < a.nw; ++k2) {
-        __syncthreads();
-        if (wave == k2) {
-#pragma unroll
-          for (int b = 0; b < DP / 32; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) jo[(b * 16 + i) * 64 + lane] = dq[b][i];
-        }
-        __syncthreads();
-        if (wave == 0) {
-#pragma unroll
-          for (int b = 0; b < DP / 32; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) dq[b][i] += jo[(b * 16 + i) * 64 + lane];
-        }
-      }
+    if constexpr (SPLIT) {
+      join_sum<DP / 32>(dq, reinterpret_cast<float*>(smem + DQ_TABLE + a.nw * wave_bytes), a.nw, wave, lane);
       if (wave) continue;
     }
     T* gq = static_cast<T*>(a.g_qkv) + (size_t)w.lo * ld + (size_t)h * a.dh;
-    if (all_finite<DP / 32>(dq, 0.f, qi < w.n)) {
-      if (qi < w.n) {
+    if (all_finite<DP / 32>(dq, 0.f, real)) {
+      if (real) {
 #pragma unroll
         for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
@@ -641,43 +736,39 @@ __global__ void __launch_bounds__(256) k_attn_dq(AttnArgs a) {
     }
     const bool d0 = lane < a.dh, d1 = lane + 64 < a.dh;
     for (int r = 0; r < PAIR_T && w.i0 + r < w.n; ++r) {
-      const size_t at = ((size_t)w.lo + w.i0 + r) * ld + (size_t)h * a.dh, og = (((size_t)w.lo + w.i0 + r) * a.nh + h) * a.dh;
-      const float q0 = d0 ? value<BF>(a.qkv, at + lane) : 0.f, q1 = d1 ? value<BF>(a.qkv, at + lane + 64) : 0.f;
+      const size_t qa = ((size_t)w.lo + w.i0 + r) * ld + (size_t)h * a.dh, og = (((size_t)w.lo + w.i0 + r) * a.nh + h) * a.dh;
+      const float q0 = d0 ? value<BF>(a.qkv, qa + lane) : 0.f, q1 = d1 ? value<BF>(a.qkv, qa + lane + 64) : 0.f;
       const float g0 = d0 ? value<BF>(a.g_out, og + lane) : 0.f, g1 = d1 ? value<BF>(a.g_out, og + lane + 64) : 0.f;
-      const float lr = __shfl(lse, r), Dr = __shfl(D, r);
+      const float mr = __shfl(st.x, r), lr = __shfl(st.y, r), Dr = __shfl(D, r);
       const uint8_t* row = w.pairs + (w.i0 + r) * w.pitch;
       float a0 = 0.f, a1 = 0.f;
       for (int j = 0; j < w.n; ++j) {
-        const float b = table[row[j]];
+        const float b = table[row[j]].x;
         if (b == -__builtin_inff()) continue;
         const size_t kj = ((size_t)w.lo + j) * ld + (size_t)(a.nh + hk) * a.dh, vj = kj + (size_t)a.nkv * a.dh;
         const float k0 = d0 ? value<BF>(a.qkv, kj + lane) : 0.f, k1 = d1 ? value<BF>(a.qkv, kj + lane + 64) : 0.f;
         const float v0 = d0 ? value<BF>(a.qkv, vj + lane) : 0.f, v1 = d1 ? value<BF>(a.qkv, vj + lane + 64) : 0.f;
-        const float p = __builtin_amdgcn_exp2f(fmaf(wave_sum(fmaf(q0, k0, q1 * k1)), a.c, b) - lr);
+        const float p = __builtin_amdgcn_exp2f(fmaf(wave_sum(fmaf(q0, k0, q1 * k1)) + b - mr, a.c, -lr));
         const float d = p * (wave_sum(fmaf(g0, v0, g1 * v1)) - Dr);
         a0 = fmaf(d, k0, a0);
         a1 = fmaf(d, k1, a1);
       }
-      if (d0) put<BF>(a.g_qkv, at + lane, a0 * a.scale);
-      if (d1) put<BF>(a.g_qkv, at + lane + 64, a1 * a.scale);
+      if (d0) put<BF>(a.g_qkv, qa + lane, a0 * a.scale);
+      if (d1) put<BF>(a.g_qkv, qa + lane + 64, a1 * a.scale);
     }
   }
 
   lds_order();
-  if (!a.split) {
-    if (me < a.per_head && lane < a.nb) a.partial[((size_t)h * a.per_head + me) * a.nb + lane] = hist_sum(hist, lane);
-    return;
-  }
-  __syncthreads();
+  if constexpr (SPLIT) __syncthreads();
   if (wave == 0 && lane < a.nb) {
     float s = 0.f;
-    for (int k2 = 0; k2 < a.nw; ++k2)
-      s += hist_sum(reinterpret_cast<const float*>(smem + k2 * wave_bytes + 1024 + tile_bytes<BF, DP>()), lane);
+    for (int k2 = 0; k2 < (SPLIT ? a.nw : 1); ++k2)
+      s += hist_sum(reinterpret_cast<const float*>(smem + DQ_TABLE + k2 * wave_bytes + 2 * tile_bytes<BF, DP>()), lane);
     a.partial[((size_t)h * a.per_head + me) * a.nb + lane] = s;
   }
 }
 
-// g_bias of head h: the wavefronts' partials in order, a run per group of threads, then the runs
+// g_bias of head h: the workgroups' partials in order, a run per group of threads, then the runs
 __device__ __forceinline__ void bias_reduce(const AttnArgs& a, int h, float* sh) {
   const int b = threadIdx.x & 63, run = threadIdx.x >> 6, runs = blockDim.x >> 6;
   const int per = (a.per_head + runs - 1) / runs, k1 = min(a.per_head, (run + 1) * per);
@@ -701,71 +792,79 @@ __device__ __forceinline__ void bias_reduce(const AttnArgs& a, int h, float* sh)
 }
 
 // -------------------------------------------------------------------------------------------------------------------------
-// g_k and g_v of 32 keys, over the query heads that share them; the last nh workgroups add up g_bias
-template <bool BF, int DP>
-__global__ void __launch_bounds__(256) k_attn_dkv(AttnArgs a, int ngroups) {
+// g_k and g_v of 32 keys, over the query heads that share them; the first nh workgroups add up g_bias
+template <bool BF, int DP, bool SPLIT>
+__global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k_attn_dkv(AttnArgs a) {
   using T = typename Row<BF, DP>::T;
   constexpr int PT = Row<BF, 32>::PITCH;
   extern __shared__ __align__(16) char smem[];
-  if ((int)blockIdx.x >= ngroups * a.nkv) {   // uniform over the workgroup
-    bias_reduce(a, blockIdx.x - ngroups * a.nkv, reinterpret_cast<float*>(smem));
+  if ((int)blockIdx.x < a.nh) {   // uniform over the workgroup
+    bias_reduce(a, blockIdx.x, reinterpret_cast<float*>(smem));
     return;
   }
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
-  const int group = blockIdx.x / a.nkv, hk = blockIdx.x - group * a.nkv;
-  const int t = a.split ? group : group * a.nw + wave;
-  if (t >= a.plan.tile_off[a.G]) return;
+  const int lane = threadIdx.x & 63, wave = SPLIT ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0, g = lane >> 5;
+  const int item = blockIdx.x - a.nh, t = item / a.nkv, hk = item - t * a.nkv;
+  if (t >= *a.plan.count) return;
   const Where w = tile_where(a, t);
-  char* mine = smem + wave * dkv_wave_bytes<BF, DP>();
-  float* table = reinterpret_cast<float*>(mine);
-  T* tq = reinterpret_cast<T*>(mine + 1024);
+  // (tables: wavefronts of one workgroup may be at different heads, so each has its own)
+  const unsigned table_at = wave * FWD_TABLE;
+  float* table = reinterpret_cast<float*>(smem + table_at);
+  T* tq = reinterpret_cast<T*>(smem + (SPLIT ? a.nw : 1) * FWD_TABLE + wave * dkv_wave_bytes<BF, DP>());
   T* tg = tq + 32 * Row<BF, DP>::PITCH;
   T* tp = tg + 32 * Row<BF, DP>::PITCH;
   T* ts = tp + 32 * PT;
   const int rep = a.nh / a.nkv;
-  const size_t ld = (size_t)(a.nh + 2 * a.nkv) * a.dh, lo_ = (size_t)a.nh * a.dh;
+  const unsigned ld = (unsigned)(a.nh + 2 * a.nkv) * a.dh, lo_ = (unsigned)a.nh * a.dh;
   const T* base = static_cast<const T*>(a.qkv) + (size_t)w.lo * ld;
   const T* gbase = static_cast<const T*>(a.g_out) + (size_t)w.lo * lo_;
   Row<BF, DP> k, v, q, go;
   {
-    const int j = w.i0 + tile_row(lane & 31);
-    const T* p = base + (size_t)(j < w.n ? j : w.n - 1) * ld + (size_t)(a.nh + hk) * a.dh;
+    const T* p = base + (size_t)(w.i0 + min(tile_row(lane & 31), w.n - 1 - w.i0)) * ld + (size_t)(a.nh + hk) * a.dh;
     k.load(p, a.dh, g);
     v.load(p + (size_t)a.nkv * a.dh, a.dh, g);
   }
   f32x16_t dk[DP / 32] = {}, dv[DP / 32] = {};
-  const int step = a.split ? a.nw * PAIR_T : PAIR_T;
-  for (int r = 0; r < rep; ++r) {
+  // the tiles of queries of one head after the other; SPLIT: dealt out in turn
+  const int step = SPLIT ? a.nw * PAIR_T : PAIR_T, span = (w.n + PAIR_T - 1) / PAIR_T * PAIR_T;
+  int i0 = wave * PAIR_T;
+  for (int r = 0; r < rep; ++r, i0 -= span) {
+    if (i0 >= span) continue;
     const int h = hk * rep + r;
     lds_order();
-    fill_table(table, a.bias + (size_t)h * a.nb, a.nb, lane);
+    fill_table(table, a.bias + (size_t)h * a.nb, a.nb, a.inv, lane);
     lds_order();
+    Tile<BF, DP> qt, gt;
     u32x4_t bk;
-    float lse, D;
+    float2 st;
+    float D;
     auto fetch = [&](int i0) {
-      const int i = i0 + (lane & 31), ic = i < w.n ? i : w.n - 1;
-      q.load(base + (size_t)ic * ld + (size_t)h * a.dh, a.dh, g);
-      go.load(gbase + (size_t)ic * lo_ + (size_t)h * a.dh, a.dh, g);
-      bk = load_buckets(w.pairs + ic * w.pitch, w.i0, w.n, g);
-      lse = i < w.n ? a.lse[(size_t)h * a.N + w.lo + i] : __builtin_inff();
-      D = a.delta[(size_t)h * a.N + w.lo + ic];
+      const bool part = i0 + 32 > w.n;
+      const unsigned il = part ? min(lane & 31, w.n - 1 - i0) : lane & 31;
+      qt.load(base + (size_t)i0 * ld + (size_t)h * a.dh, ld, w.n - i0, a.dh, lane);
+      gt.load(gbase + (size_t)i0 * lo_ + (size_t)h * a.dh, lo_, w.n - i0, a.dh, lane);
+      bk = load_buckets(w.pairs + i0 * w.pitch + w.i0 + (il * (unsigned)w.pitch + 16 * g), w.i0, w.n, g);
+      const size_t at = (size_t)h * a.N + w.lo + i0;
+      st = a.stat[at + il];
+      D = a.delta[at + il];
+      if (part && (lane & 31) > (int)il) st = make_float2(0.f, __builtin_inff());   // a row past the last atom: weight 0
     };
-    int i0 = a.split ? wave * PAIR_T : 0;
-    if (i0 < w.n) fetch(i0);
+    fetch(i0);
     for (; i0 < w.n; i0 += step) {
-      f32x16_t s = Row<BF, DP>::dot(k, q), ds = Row<BF, DP>::dot(v, go);
       lds_order();
-      q.to_lds(tq + (lane & 31) * Row<BF, DP>::PITCH, g);
-      go.to_lds(tg + (lane & 31) * Row<BF, DP>::PITCH, g);
-      const u32x4_t bc = bk;
-      const float lc = lse, Dc = D;
+      qt.to_lds(tq, lane);
+      gt.to_lds(tg, lane);
+      f32x16_t s = biases(table_at, bk);
+      lds_order();
+      const float2 sc = st;
+      const float Dc = D;
       if (i0 + step < w.n) fetch(i0 + step);
+      q.from_lds(tq, lane & 31, g);
+      s = Row<BF, DP>::dot(k, q, s);
+      go.from_lds(tg, lane & 31, g);
+      f32x16_t ds = Row<BF, DP>::dot(v, go, f32x16_t{});
+      weights_of(s, a.c, sc.x, sc.y);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, table[bucket_of(bc, i)]) - lc);
-        s[i] = p;
-        ds[i] = p * (ds[i] - Dc);
-      }
+      for (int i = 0; i < 16; ++i) ds[i] = s[i] * (ds[i] - Dc);
       weights_to_lds<BF>(Weights<BF>(s), tp, lane);
       weights_to_lds<BF>(Weights<BF>(ds), ts, lane);
       lds_order();
@@ -773,28 +872,10 @@ __global__ void __launch_bounds__(256) k_attn_dkv(AttnArgs a, int ngroups) {
       add_cols_lds<BF, DP>(tq, ts, dk, lane);
     }
   }
-  if (a.split) {
-    float* jo = reinterpret_cast<float*>(smem + a.nw * dkv_wave_bytes<BF, DP>());
-    for (int k2 = 1; k2 < a.nw; ++k2) {
-#pragma unroll
-      for (int which = 0; which < 2; ++which) {
-        f32x16_t(&x)[DP / 32] = which ? dv : dk;
-        __syncthreads();
-        if (wave == k2) {
-#pragma unroll
-          for (int b = 0; b < DP / 32; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) jo[(b * 16 + i) * 64 + lane] = x[b][i];
-        }
-        __syncthreads();
-        if (wave == 0) {
-#pragma unroll
-          for (int b = 0; b < DP / 32; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[b][i] += jo[(b * 16 + i) * 64 + lane];
-        }
-      }
-    }
+  if constexpr (SPLIT) {
+    float* room = reinterpret_cast<float*>(smem + a.nw * (FWD_TABLE + dkv_wave_bytes<BF, DP>()));
+    join_sum<DP / 32>(dk, room, a.nw, wave, lane);
+    join_sum<DP / 32>(dv, room, a.nw, wave, lane);
     if (wave) return;
   }
   const int kj = w.i0 + (lane & 31);
@@ -824,7 +905,7 @@ __global__ void __launch_bounds__(256) k_attn_dkv(AttnArgs a, int ngroups) {
     for (int u = 0; u < rep; ++u) {
       const int h = hk * rep + u;
       lds_order();
-      fill_table(table, a.bias + (size_t)h * a.nb, a.nb, lane);
+      fill_table(table, a.bias + (size_t)h * a.nb, a.nb, a.inv, lane);
       lds_order();
       for (int i = 0; i < w.n; ++i) {
         const float b = table[w.pairs[i * w.pitch + w.i0 + r]];
@@ -832,7 +913,8 @@ __global__ void __launch_bounds__(256) k_attn_dkv(AttnArgs a, int ngroups) {
         const size_t qa = ((size_t)w.lo + i) * ld + (size_t)h * a.dh, ga = (((size_t)w.lo + i) * a.nh + h) * a.dh;
         const float q0 = d0 ? value<BF>(a.qkv, qa + lane) : 0.f, q1 = d1 ? value<BF>(a.qkv, qa + lane + 64) : 0.f;
         const float g0 = d0 ? value<BF>(a.g_out, ga + lane) : 0.f, g1 = d1 ? value<BF>(a.g_out, ga + lane + 64) : 0.f;
-        const float p = __builtin_amdgcn_exp2f(fmaf(wave_sum(fmaf(q0, k0, q1 * k1)), a.c, b) - a.lse[(size_t)h * a.N + w.lo + i]);
+        const float2 st = a.stat[(size_t)h * a.N + w.lo + i];
+        const float p = __builtin_amdgcn_exp2f(fmaf(wave_sum(fmaf(q0, k0, q1 * k1)) + b - st.x, a.c, -st.y));
         const float d = p * (wave_sum(fmaf(g0, v0, g1 * v1)) - a.delta[(size_t)h * a.N + w.lo + i]);
         a0 = fmaf(d, q0, a0);
         a1 = fmaf(d, q1, a1);
@@ -849,11 +931,11 @@ __global__ void __launch_bounds__(256) k_attn_dkv(AttnArgs a, int ngroups) {
 constexpr int LDS_MOST = 64 * 1024;   // of a workgroup, so that two fit a compute unit and no attribute has to be set
 
 int waves_that_fit(int wave_bytes, int extra) {
-  int nw = (LDS_MOST - extra) / wave_bytes;
+  const int nw = (LDS_MOST - extra) / wave_bytes;
   return nw >= 4 ? 4 : nw >= 2 ? 2 : 1;
 }
 
-// wavefronts per head of the reverse kernel over queries: every tile its own while they are few, then as many as keep the chip
+// workgroups per head of the reverse kernel over queries: every tile its own while they are few, then as many as keep the chip
 // busy (each leaves one partial of g_bias)
 int64_t dq_per_head(int64_t max_tiles, int nh) {
   const int64_t most = (4096 + nh - 1) / nh;
@@ -873,13 +955,14 @@ AttnWs carve_attn_ws(void* p, int N, int G, int nh, int nb) {
   return w;
 }
 struct AttnSaved {
-  float *lse, *o32;
+  float2* stat;
+  float* o32;
   size_t bytes;
 };
 AttnSaved carve_attn_saved(void* p, int N, int nh, int dh, bool bf16) {
   Carver c(p);
   AttnSaved s;
-  s.lse = c.take<float>((size_t)nh * N);
+  s.stat = c.take<float2>((size_t)nh * N);
   s.o32 = bf16 ? c.take<float>((size_t)N * nh * dh) : nullptr;
   s.bytes = c.used();
   return s;
@@ -897,46 +980,63 @@ int32_t check_attn(int32_t N, int32_t G, int32_t nh, int32_t nkv, int32_t dh, in
   return HGNN_OK;
 }
 
-// Few tiles: the wavefronts of a workgroup share one tile and deal out the other side's. Until there is a wavefront per SIMD
-// this shortens the chain of tiles without taking a compute unit from anybody.
-bool attn_split(int64_t max_tiles, int nh, int G, int N) { return max_tiles * nh <= 4 * num_cus() && N > 2 * PAIR_T * (int64_t)G; }
+// The wavefronts of a workgroup share a tile of rows and deal out the other side's tiles in two cases. Few tiles: until there is a
+// wavefront per SIMD this shortens the chain of tiles without taking a compute unit from anybody. Long graphs: 2,500
+// wavefronts of 625 tiles each leave a fifth of the SIMDs idle at the end; four times as many of a quarter the length do not, and
+// the join is small against their chains.
+// Where keys are shared by query heads, k_attn_dkv has few and long chains as well.
+bool attn_split(int64_t max_tiles, int heads, int64_t G, int64_t N, int rep) {
+  return (max_tiles * heads <= 4 * num_cus() && N * rep > 2 * PAIR_T * G) || N >= 1024 * G || rep > 1;
+}
 
-template <bool BF, int DP>
+template <bool BF, int DP, bool SPLIT>
 int32_t launch_fwd(hipStream_t st, AttnArgs a) {
-  constexpr int WB = fwd_wave_bytes<BF, DP>();
-  a.split = attn_split(a.plan.max_tiles, a.nh, a.G, a.N);
-  const int extra = a.split ? join_bytes(DP) : 0;
-  a.nw = waves_that_fit(WB, extra);
-  const int64_t groups = a.split ? a.plan.max_tiles : (a.plan.max_tiles + a.nw - 1) / a.nw;
-  k_attn_fwd<BF, DP><<<(unsigned)(groups * a.nh), 64 * a.nw, WB * a.nw + extra, st>>>(a);
+  const int extra = FWD_TABLE + (SPLIT ? join_bytes(DP) : 0);
+  constexpr int WB = 2 * tile_bytes<BF, DP>();
+  a.nw = SPLIT ? waves_that_fit(WB, extra) : 1;
+  k_attn_fwd<BF, DP, SPLIT><<<(unsigned)(a.plan.max_tiles * a.nh), 64 * a.nw, WB * a.nw + extra, st>>>(a);
   HGNN_LAUNCH_CHECK("k_attn_fwd");
   return HGNN_OK;
 }
 
-template <bool BF, int DP>
-int32_t launch_bwd(hipStream_t st, AttnArgs a) {
-  a.split = attn_split(a.plan.max_tiles, a.nh, a.G, a.N);
-  {
-    const int wb = dq_wave_bytes<BF, DP>(a.nb), extra = a.split ? join_bytes(DP) : 0;
-    a.nw = a.split ? waves_that_fit(wb, extra) : 1;   // (nothing is shared but in a split tile, and single wavefronts pack into LDS best)
-    const int64_t groups = a.split ? a.per_head : (a.per_head + a.nw - 1) / a.nw;
-    k_attn_dq<BF, DP><<<(unsigned)(groups * a.nh), 64 * a.nw, wb * a.nw + extra, st>>>(a);
-    HGNN_LAUNCH_CHECK("k_attn_dq");
-  }
-  constexpr int WB = dkv_wave_bytes<BF, DP>();
-  const int extra = a.split ? join_bytes(DP) : 0;
-  a.nw = waves_that_fit(WB, extra);
-  const int64_t groups = a.split ? a.plan.max_tiles : (a.plan.max_tiles + a.nw - 1) / a.nw;
-  k_attn_dkv<BF, DP><<<(unsigned)(groups * a.nkv + a.nh), 64 * a.nw, WB * a.nw + extra, st>>>(a, (int)groups);
+template <bool BF, int DP, bool SPLIT>
+int32_t launch_dq(hipStream_t st, AttnArgs a) {
+  const int wb = dq_wave_bytes<BF, DP>(a.nb), extra = DQ_TABLE + (SPLIT ? join_bytes(DP) : 0);
+  a.nw = SPLIT ? waves_that_fit(wb, extra) : 1;
+  k_attn_dq<BF, DP, SPLIT><<<(unsigned)((int64_t)a.per_head * a.nh), 64 * a.nw, wb * a.nw + extra, st>>>(a);
+  HGNN_LAUNCH_CHECK("k_attn_dq");
+  return HGNN_OK;
+}
+
+template <bool BF, int DP, bool SPLIT>
+int32_t launch_dkv(hipStream_t st, AttnArgs a) {
+  constexpr int WB = FWD_TABLE + dkv_wave_bytes<BF, DP>();
+  const int extra = SPLIT ? join_bytes(DP) : 0;
+  a.nw = SPLIT ? waves_that_fit(WB, extra) : 1;
+  k_attn_dkv<BF, DP, SPLIT><<<(unsigned)(a.plan.max_tiles * a.nkv + a.nh), 64 * a.nw, WB * a.nw + extra, st>>>(a);
   HGNN_LAUNCH_CHECK("k_attn_dkv");
   return HGNN_OK;
 }
 
+template <bool BF, int DP>
+int32_t run_width(hipStream_t st, const AttnArgs& a, bool fwd) {
+  const bool split = attn_split(a.plan.max_tiles, a.nh, a.G, a.N, 1);
+  if (fwd) return split ? launch_fwd<BF, DP, true>(st, a) : launch_fwd<BF, DP, false>(st, a);
+  HGNN_TRY((split ? launch_dq<BF, DP, true>(st, a) : launch_dq<BF, DP, false>(st, a)));
+  return attn_split(a.plan.max_tiles, a.nkv, a.G, a.N, a.nh / a.nkv) ? launch_dkv<BF, DP, true>(st, a) : launch_dkv<BF, DP, false>(st, a);
+}
+
 template <bool BF>
 int32_t run_attn(hipStream_t st, const AttnArgs& a, bool fwd) {
-  if (a.dh <= 32) return fwd ? launch_fwd<BF, 32>(st, a) : launch_bwd<BF, 32>(st, a);
-  if (a.dh <= 64) return fwd ? launch_fwd<BF, 64>(st, a) : launch_bwd<BF, 64>(st, a);
-  return fwd ? launch_fwd<BF, 128>(st, a) : launch_bwd<BF, 128>(st, a);
+  if (a.dh <= 32) return run_width<BF, 32>(st, a, fwd);
+  if (a.dh <= 64) return run_width<BF, 64>(st, a, fwd);
+  return run_width<BF, 128>(st, a, fwd);
+}
+
+// (scores are kept in units of the product, biases divided by the scale)
+int32_t check_scale(float scale) {
+  HGNN_REQUIRE(scale >= 1e-6f && scale <= 1e6f, HGNN_ERR_BAD_SHAPE, "graph_attention: the scale must be in 1e-6..1e6 (got %g)", (double)scale);
+  return HGNN_OK;
 }
 
 __global__ void k_zero_bias(float* p, int n) {
@@ -962,6 +1062,7 @@ extern "C" int32_t hgnn_graph_attention_fwd(void* stream, int32_t N, int32_t G, 
                                             int32_t dtype, float scale, const void* plan, size_t plan_bytes, const uint8_t* pairs,
                                             const void* qkv, const float* bias, void* out, void* saved, size_t saved_bytes) {
   HGNN_TRY(check_attn(N, G, nh, nkv, dh, nb, dtype));
+  HGNN_TRY(check_scale(scale));
   if (N == 0) return HGNN_OK;
   HGNN_REQUIRE(plan && pairs && qkv && bias && out, HGNN_ERR_NULLPTR, "graph_attention_fwd: null pointer");
   AttnArgs a{};
@@ -971,9 +1072,9 @@ extern "C" int32_t hgnn_graph_attention_fwd(void* stream, int32_t N, int32_t G, 
   HGNN_REQUIRE(!saved || saved_bytes >= s.bytes, HGNN_ERR_WORKSPACE_TOO_SMALL, "graph_attention saved buffer: need %zu bytes, got %zu", s.bytes, saved_bytes);
   if (a.plan.max_tiles == 0) return HGNN_OK;   // (G == 0: no plan of N atoms exists)
   a.N = N; a.G = G; a.nh = nh; a.nkv = nkv; a.dh = dh; a.nb = nb;
-  a.scale = scale; a.c = scale * LOG2E;
+  a.scale = scale; a.c = scale * LOG2E; a.inv = 1.0f / scale;
   a.pairs = pairs; a.qkv = qkv; a.bias = bias; a.out = out;
-  a.lse = saved ? s.lse : nullptr;
+  a.stat = saved ? s.stat : nullptr;
   a.o32 = saved ? s.o32 : nullptr;
   hipStream_t st = static_cast<hipStream_t>(stream);
   ProfScope ps(PT_MISC, st);
@@ -985,6 +1086,7 @@ extern "C" int32_t hgnn_graph_attention_bwd(void* stream, int32_t N, int32_t G, 
                                             const void* qkv, const float* bias, const void* out, const void* saved, size_t saved_bytes,
                                             const void* g_out, void* g_qkv, float* g_bias, void* ws, size_t ws_bytes) {
   HGNN_TRY(check_attn(N, G, nh, nkv, dh, nb, dtype));
+  HGNN_TRY(check_scale(scale));
   HGNN_REQUIRE(g_bias, HGNN_ERR_NULLPTR, "graph_attention_bwd: null pointer");
   hipStream_t st = static_cast<hipStream_t>(stream);
   AttnArgs a{};
@@ -1002,8 +1104,8 @@ extern "C" int32_t hgnn_graph_attention_bwd(void* stream, int32_t N, int32_t G, 
   HGNN_REQUIRE(ws_bytes >= w.bytes, HGNN_ERR_WORKSPACE_TOO_SMALL, "graph_attention workspace: need %zu bytes, got %zu", w.bytes, ws_bytes);
   a.N = N; a.G = G; a.nh = nh; a.nkv = nkv; a.dh = dh; a.nb = nb;
   a.per_head = (int)dq_per_head(a.plan.max_tiles, nh);
-  a.scale = scale; a.c = scale * LOG2E;
-  a.pairs = pairs; a.qkv = qkv; a.bias = bias; a.out = const_cast<void*>(out); a.lse = s.lse; a.o32 = s.o32;
+  a.scale = scale; a.c = scale * LOG2E; a.inv = 1.0f / scale;
+  a.pairs = pairs; a.qkv = qkv; a.bias = bias; a.out = const_cast<void*>(out); a.stat = s.stat; a.o32 = s.o32;
   a.g_out = g_out; a.g_qkv = g_qkv; a.delta = w.delta; a.partial = w.partial; a.g_bias = g_bias;
   ProfScope ps(PT_MISC, st);
   return dtype == HGNN_BF16 ? run_attn<true>(st, a, false) : run_attn<false>(st, a, false);

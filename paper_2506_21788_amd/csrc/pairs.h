@@ -9,11 +9,20 @@ namespace hgnn {
 
 constexpr int PAIR_T = 32;   // atoms of a tile: the edge of a matrix-core tile
 
+// What a kernel has to know of a tile, in one load: with the graph's number alone its place took two more, each waiting for the one
+// before (attention over 390 structures, 13,000 wavefronts of a few tiles each: see k_attn_fwd)
+struct alignas(32) PairTile {
+  int64_t off;        // first byte of the graph's matrix
+  int32_t lo, n;      // the graph's first atom, its atoms
+  int32_t i0, g;      // first atom of the tile within the graph, the graph
+  int32_t unused[2];
+};
+
 struct PairPlan {
-  int64_t* pair_off;      // [G+1] first byte of every graph's matrix
-  int32_t* graph_off;     // [G+1] first atom of every graph (checked)
-  int32_t* tile_off;      // [G+1] tiles of PAIR_T atoms before every graph; [G] = tiles in all, 0 if the offsets were refused
-  int32_t* tile_graph;    // [max_tiles] graph of every tile
+  int32_t* count;         // [1] tiles in all; 0 if the offsets were refused
+  int64_t* pair_off;      // [G] first byte of every graph's matrix
+  int32_t* tile_off;      // [G+1] tiles of PAIR_T atoms before every graph
+  PairTile* tile;         // [max_tiles]
   int64_t max_tiles;      // what N atoms in G graphs can at most make
   size_t bytes;
 };
@@ -22,10 +31,10 @@ inline PairPlan pair_plan_view(const void* plan, int32_t N, int32_t G) {
   Carver c(const_cast<void*>(plan));
   PairPlan v;
   v.max_tiles = (int64_t)N / PAIR_T + (G < N ? G : N);
-  v.pair_off = c.take<int64_t>((size_t)G + 1);
-  v.graph_off = c.take<int32_t>((size_t)G + 1);
+  v.count = c.take<int32_t>(1);
+  v.pair_off = c.take<int64_t>((size_t)G);
   v.tile_off = c.take<int32_t>((size_t)G + 1);
-  v.tile_graph = c.take<int32_t>((size_t)v.max_tiles);
+  v.tile = c.take<PairTile>((size_t)v.max_tiles);
   v.bytes = c.used();
   return v;
 }

@@ -58,7 +58,6 @@ __global__ void __launch_bounds__(1024) k_pair_plan(int N, int G, const int32_t*
     if (g < G) {
       v.pair_off[g] = pb + ib - bytes;
       v.tile_off[g] = pt + it - tiles;
-      v.graph_off[g] = graph_off[g];
     }
     base_b += tb;
     base_t += tt;
@@ -67,24 +66,29 @@ __global__ void __launch_bounds__(1024) k_pair_plan(int N, int G, const int32_t*
   if (bad) atomicOr(&bad_s, 1);
   __syncthreads();
   if (tid == 0) {
-    v.pair_off[G] = bad_s ? 0 : base_b;
-    v.graph_off[G] = N;
-    v.tile_off[G] = bad_s ? 0 : base_t;
+    v.tile_off[G] = base_t;
+    *v.count = bad_s ? 0 : base_t;
     post_mail(mail, base_b, bad_s);
   }
 }
 
-// the graph of every tile: a binary search per tile
-__global__ void __launch_bounds__(256) k_pair_tiles(int G, PairPlan v) {
+// every tile's record: a binary search for its graph
+__global__ void __launch_bounds__(256) k_pair_tiles(int G, const int32_t* graph_off, PairPlan v) {
   const int t = blockIdx.x * 256 + threadIdx.x;
-  if (t >= v.tile_off[G]) return;
+  if (t >= *v.count) return;
   int lo = 0, hi = G;   // tile_off[lo] <= t < tile_off[hi]
   while (hi - lo > 1) {
     const int m = (lo + hi) >> 1;
     if (v.tile_off[m] <= t) lo = m;
     else hi = m;
   }
-  v.tile_graph[t] = lo;
+  PairTile r{};
+  r.off = v.pair_off[lo];
+  r.lo = graph_off[lo];
+  r.n = graph_off[lo + 1] - r.lo;
+  r.i0 = (t - v.tile_off[lo]) * PAIR_T;
+  r.g = lo;
+  v.tile[t] = r;
 }
 
 struct BucketArgs {
@@ -100,10 +104,9 @@ __global__ void __launch_bounds__(256) k_pair_buckets(BucketArgs a) {
   __shared__ float4 img[27];
   __shared__ float edge[PAIR_EDGES + 1];
   const int tile = blockIdx.x >> 2;
-  if (tile >= a.plan.tile_off[a.G]) return;
-  const int g = a.plan.tile_graph[tile];
-  const int lo = a.plan.graph_off[g], n = a.plan.graph_off[g + 1] - lo;
-  const int i0 = (tile - a.plan.tile_off[g]) * PAIR_T + (blockIdx.x & 3) * 8;
+  if (tile >= *a.plan.count) return;
+  const PairTile w = a.plan.tile[tile];
+  const int g = w.g, lo = w.lo, n = w.n, i0 = w.i0 + (blockIdx.x & 3) * 8;
   if (i0 >= n) return;
   const bool periodic = a.cell && a.pbc && a.pbc[g];
   if (threadIdx.x < 27) {
@@ -124,7 +127,7 @@ __global__ void __launch_bounds__(256) k_pair_buckets(BucketArgs a) {
   const float* p = a.pos + ((size_t)lo + i) * 3;
   const float px = p[0], py = p[1], pz = p[2];
   const int64_t pitch = pair_pitch(n);
-  uint8_t* row = a.pairs + a.plan.pair_off[g] + i * pitch;
+  uint8_t* row = a.pairs + w.off + i * pitch;
   const int first = periodic ? 0 : 13, last = periodic ? 26 : 13;
   for (int j = (threadIdx.x & 31) * 4; j < pitch; j += 128) {
     float q[4][3], best[4];
@@ -191,7 +194,7 @@ extern "C" int32_t hgnn_pair_plan(void* stream, int32_t N, int32_t G, const int3
     k_pair_plan<<<1, 1024, 0, st>>>(N, G, graph_off, v, mail.dev());
     HGNN_LAUNCH_CHECK("k_pair_plan");
     if (v.max_tiles > 0) {
-      k_pair_tiles<<<(unsigned)((v.max_tiles + 255) / 256), 256, 0, st>>>(G, v);
+      k_pair_tiles<<<(unsigned)((v.max_tiles + 255) / 256), 256, 0, st>>>(G, graph_off, v);
       HGNN_LAUNCH_CHECK("k_pair_tiles");
     }
   }

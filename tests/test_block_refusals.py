@@ -67,11 +67,12 @@ def test_graph_attention():
                      (dict(dt=2), SHAPE), (dict(N=1 << 28), OVERFLOW), (dict(N=200_000_000, G=100_000_000, nh=64, kv=1), OVERFLOW)):
         assert size(**kw) == code, kw
 
-    def fwd(N=100, plan=P, pb=1 << 20, pairs=P, qkv=P, bias=P, out=P, saved=None, sb=0):
-        return lib.hgnn_graph_attention_fwd(None, i32(N), i32(3), i32(4), i32(2), i32(32), i32(8), i32(0), f32(1.0), plan, sz(pb), pairs, qkv, bias,
+    def fwd(N=100, plan=P, pb=1 << 20, pairs=P, qkv=P, bias=P, out=P, saved=None, sb=0, scale=1.0):
+        return lib.hgnn_graph_attention_fwd(None, i32(N), i32(3), i32(4), i32(2), i32(32), i32(8), i32(0), f32(scale), plan, sz(pb), pairs, qkv, bias,
                                             out, saved, sz(sb))
     for kw, code in ((dict(plan=None), NULL), (dict(pairs=None), NULL), (dict(qkv=None), NULL), (dict(bias=None), NULL), (dict(out=None), NULL),
-                     (dict(pb=64), WS), (dict(saved=P, sb=64), WS), (dict(N=0, qkv=None), 0)):
+                     (dict(pb=64), WS), (dict(saved=P, sb=64), WS), (dict(N=0, qkv=None), 0), (dict(scale=0.0), SHAPE), (dict(scale=-1.0), SHAPE),
+                     (dict(scale=float("nan")), SHAPE), (dict(scale=float("inf")), SHAPE)):
         assert fwd(**kw) == code, kw
 
     def bwd(pb=1 << 20, saved=P, sb=1 << 20, g=P, gq=P, gb=P, ws=P, wb=1 << 20, out=P):

@@ -191,6 +191,20 @@ def test_biases_of_the_lowest_value_and_of_minus_infinity(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("far", [-1e9, float(np.finfo(np.float32).min)])
+def test_gradients_of_rows_of_far_biases(far, dtype):
+    """Every bias of a head at one far value: at that size float32 holds no score, the weights are equal, forward and reverse."""
+    P = _problem([45, 80], 2, 1, 16, 1, dtype, holes=False)
+    P["bias"] = np.full((2, 1), far)
+    P["qkv"] = np.concatenate([np.zeros_like(P["qkv"][:, :2]), P["qkv"][:, 2:]], 1)      # scores of zero: exactly the same weights
+    got = _run(P)
+    P["bias"] = np.zeros((2, 1))
+    want = ob.graph_attention(P["qkv"], P["bias"], P["pairs"], P["off"], 2, 1, P["scale"], P["g"])
+    for a, w, t in zip(got, want, _allowed(P, *want)):
+        assert (np.abs(a - w) <= t + 1e-37).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_large_scores(dtype):
     """Scores of some hundred: one weight of a row is nearly 1, the others vanish."""
     P = _problem([64, 100], 2, 2, 32, 4, dtype)
