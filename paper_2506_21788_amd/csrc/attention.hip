@@ -44,6 +44,7 @@ struct AttnArgs {
   int N, G, nh, nkv, dh, nb;
   int nw;        // wavefronts of a workgroup: 1, or (SPLIT) those that share a tile of rows and deal out the other side's tiles
   int per_head;  // workgroups per head of k_attn_dq
+  int near;      // see item_of
   float scale, c, inv;   // c = scale log2 e, inv = 1 / scale
   PairPlan plan;
   const uint8_t* pairs;
@@ -404,6 +405,24 @@ __device__ __forceinline__ bool all_finite(const f32x16_t (&acc)[NB], float more
   return __all(!counts || z == 0.f);
 }
 
+// Item of a workgroup: tile (or share of the tiles) i and head h of `heads`. Workgroups are dealt to the 8 XCDs in turn. near: ITEM_TILES
+// consecutive tiles with all their heads go to one XCD, so that the heads of an atom, parts of one line of qkv, out and the
+// gradients, meet in one L2 (the next to the next XCD: graphs may be sorted by size). Else, in long graphs, the heads of a tile
+// go to different XCDs: each gets few heads, whose keys and values its L2 can hold.
+constexpr unsigned ITEM_TILES = 4;
+__device__ __forceinline__ void item_of(int near, unsigned block, unsigned heads, int& i, int& h) {
+  if (near) {
+    const unsigned place = block >> 3, run = place / (ITEM_TILES * heads), r = place - run * (ITEM_TILES * heads);
+    i = (run * 8 + (block & 7)) * ITEM_TILES + r / heads;
+    h = r % heads;
+  } else {
+    i = block / heads;
+    h = block - i * heads;
+  }
+}
+// workgroups for n items a head
+int64_t item_blocks(int near, int64_t n, int heads) { return near ? (n + 8 * ITEM_TILES - 1) / (8 * ITEM_TILES) * (8 * ITEM_TILES) * heads : n * heads; }
+
 // where a workgroup's rows are (t: uniform)
 struct Where {
   int lo, n, i0;           // the graph's first atom, its atoms, first row of the tile
@@ -458,8 +477,10 @@ __global__ void __launch_bounds__(256, DP == 128 ? 1 : 2) k_attn_fwd(AttnArgs a)
   using T = typename Row<BF, DP>::T;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x & 63, wave = SPLIT ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0, g = lane >> 5;
-  const int t = blockIdx.x / a.nh, h = blockIdx.x - t * a.nh;
-  if (t >= *a.plan.count) return;   // uniform over the workgroup
+  const int ntiles = *a.plan.count;
+  int t, h;
+  item_of(a.near, blockIdx.x, a.nh, t, h);
+  if (t >= ntiles) return;   // uniform over the workgroup
   const Where w = tile_where(a, t);
   float* table = reinterpret_cast<float*>(smem);
   T* tk = reinterpret_cast<T*>(smem + FWD_TABLE + wave * 2 * tile_bytes<BF, DP>());
@@ -611,21 +632,22 @@ __device__ __forceinline__ float hist_sum(const float* hist, int b) {
   return ((s[0] + s[4]) + (s[1] + s[5])) + ((s[2] + s[6]) + (s[3] + s[7]));
 }
 
-// adds x[k] to this lane's word at LDS address at[k], HB words at a time: they are read together, and one that is named twice
-// takes up what the earlier one has made of it. (Adding in LDS itself, ds_add_f32, took 210 cycles of the compute unit for 64 words.)
-constexpr int HB = 4;
-__device__ __forceinline__ void hist_add(const unsigned (&at)[HB], const float (&x)[HB]) {
-  float v[HB];
+// Adds to this lane's words of LDS, HB at a time: they are read together, and one that is named twice takes up what the earlier
+// one has made of it. (Adding in LDS itself, ds_add_f32, took 210 cycles of the compute unit for 64 words.)
+constexpr int HB = 2;
+__device__ __forceinline__ void hist_read(const unsigned (&at)[16], int i, float (&v)[HB]) {
 #pragma unroll
-  for (int k = 0; k < HB; ++k) v[k] = lds<float>(at[k]);
+  for (int k = 0; k < HB; ++k) v[k] = lds<float>(at[i + k]);
+}
+__device__ __forceinline__ void hist_add(const unsigned (&at)[16], int i, float (&v)[HB], const f32x16_t& x) {
 #pragma unroll
   for (int k = 0; k < HB; ++k) {
 #pragma unroll
-    for (int u = 0; u < k; ++u) v[k] = at[k] == at[u] ? v[u] : v[k];
-    v[k] += x[k];
+    for (int u = 0; u < k; ++u) v[k] = at[i + k] == at[i + u] ? v[u] : v[k];
+    v[k] += x[i + k];
   }
 #pragma unroll
-  for (int k = 0; k < HB; ++k) lds<float>(at[k]) = v[k];
+  for (int k = 0; k < HB; ++k) lds<float>(at[i + k]) = v[k];
 }
 
 // -------------------------------------------------------------------------------------------------------------------------
@@ -635,7 +657,9 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k
   using T = typename Row<BF, DP>::T;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x & 63, wave = SPLIT ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0, g = lane >> 5;
-  const int me = blockIdx.x / a.nh, h = blockIdx.x - me * a.nh;
+  int me, h;
+  item_of(a.near, blockIdx.x, a.nh, me, h);
+  if (me >= a.per_head) return;   // uniform over the workgroup
   const int wave_bytes = dq_wave_bytes<BF, DP>(a.nb);
   float2* table = reinterpret_cast<float2*>(smem);
   T* tk = reinterpret_cast<T*>(smem + DQ_TABLE + wave * wave_bytes);
@@ -704,18 +728,18 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k
       s = Row<BF, DP>::dot(k, q, s);
       v.from_lds(tv, tile_row(lane & 31), g);
       f32x16_t ds = Row<BF, DP>::dot(v, go, f32x16_t{});
+      // (the first words of the sums of g_bias are on their way while the weights are formed, the next while the ones before are added)
+      float v4[HB];
+      hist_read(at, 0, v4);
       weights_of(s, a.c, st.x, st.y);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) ds[i] = s[i] * (ds[i] - D);
-      add_cols<BF, DP>(tk, Weights<BF>(ds), dq, lane);
-#pragma unroll
       for (int i = 0; i < 16; i += HB) {
-        unsigned ha[HB];
-        float x[HB];
 #pragma unroll
-        for (int u = 0; u < HB; ++u) { ha[u] = at[i + u]; x[u] = ds[i + u]; }
-        hist_add(ha, x);
+        for (int u = 0; u < HB; ++u) ds[i + u] = s[i + u] * (ds[i + u] - D);
+        hist_add(at, i, v4, ds);
+        if (i + HB < 16) hist_read(at, i + HB, v4);
       }
+      add_cols<BF, DP>(tk, Weights<BF>(ds), dq, lane);
     }
     if constexpr (SPLIT) {
       join_sum<DP / 32>(dq, reinterpret_cast<float*>(smem + DQ_TABLE + a.nw * wave_bytes), a.nw, wave, lane);
@@ -803,8 +827,11 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k
     return;
   }
   const int lane = threadIdx.x & 63, wave = SPLIT ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0, g = lane >> 5;
-  const int item = blockIdx.x - a.nh, t = item / a.nkv, hk = item - t * a.nkv;
-  if (t >= *a.plan.count) return;
+  const int ntiles = *a.plan.count;
+  const unsigned item = blockIdx.x - a.nh;
+  int t, hk;
+  item_of(a.near, item, a.nkv, t, hk);
+  if (t >= ntiles) return;
   const Where w = tile_where(a, t);
   // (tables: wavefronts of one workgroup may be at different heads, so each has its own)
   const unsigned table_at = wave * FWD_TABLE;
@@ -994,7 +1021,7 @@ int32_t launch_fwd(hipStream_t st, AttnArgs a) {
   const int extra = FWD_TABLE + (SPLIT ? join_bytes(DP) : 0);
   constexpr int WB = 2 * tile_bytes<BF, DP>();
   a.nw = SPLIT ? waves_that_fit(WB, extra) : 1;
-  k_attn_fwd<BF, DP, SPLIT><<<(unsigned)(a.plan.max_tiles * a.nh), 64 * a.nw, WB * a.nw + extra, st>>>(a);
+  k_attn_fwd<BF, DP, SPLIT><<<(unsigned)item_blocks(a.near, a.plan.max_tiles, a.nh), 64 * a.nw, WB * a.nw + extra, st>>>(a);
   HGNN_LAUNCH_CHECK("k_attn_fwd");
   return HGNN_OK;
 }
@@ -1003,7 +1030,7 @@ template <bool BF, int DP, bool SPLIT>
 int32_t launch_dq(hipStream_t st, AttnArgs a) {
   const int wb = dq_wave_bytes<BF, DP>(a.nb), extra = DQ_TABLE + (SPLIT ? join_bytes(DP) : 0);
   a.nw = SPLIT ? waves_that_fit(wb, extra) : 1;
-  k_attn_dq<BF, DP, SPLIT><<<(unsigned)((int64_t)a.per_head * a.nh), 64 * a.nw, wb * a.nw + extra, st>>>(a);
+  k_attn_dq<BF, DP, SPLIT><<<(unsigned)item_blocks(a.near, a.per_head, a.nh), 64 * a.nw, wb * a.nw + extra, st>>>(a);
   HGNN_LAUNCH_CHECK("k_attn_dq");
   return HGNN_OK;
 }
@@ -1013,13 +1040,15 @@ int32_t launch_dkv(hipStream_t st, AttnArgs a) {
   constexpr int WB = FWD_TABLE + dkv_wave_bytes<BF, DP>();
   const int extra = SPLIT ? join_bytes(DP) : 0;
   a.nw = SPLIT ? waves_that_fit(WB, extra) : 1;
-  k_attn_dkv<BF, DP, SPLIT><<<(unsigned)(a.plan.max_tiles * a.nkv + a.nh), 64 * a.nw, WB * a.nw + extra, st>>>(a);
+  k_attn_dkv<BF, DP, SPLIT><<<(unsigned)(item_blocks(a.near, a.plan.max_tiles, a.nkv) + a.nh), 64 * a.nw, WB * a.nw + extra, st>>>(a);
   HGNN_LAUNCH_CHECK("k_attn_dkv");
   return HGNN_OK;
 }
 
 template <bool BF, int DP>
-int32_t run_width(hipStream_t st, const AttnArgs& a, bool fwd) {
+int32_t run_width(hipStream_t st, AttnArgs a, bool fwd) {
+  // (the keys and values of a graph of average length against the L2 of an XCD, 4 MB)
+  a.near = 2.0 * a.N / a.G * a.nkv * a.dh * (BF ? 2 : 4) <= 2e6;
   const bool split = attn_split(a.plan.max_tiles, a.nh, a.G, a.N, 1);
   if (fwd) return split ? launch_fwd<BF, DP, true>(st, a) : launch_fwd<BF, DP, false>(st, a);
   HGNN_TRY((split ? launch_dq<BF, DP, true>(st, a) : launch_dq<BF, DP, false>(st, a)));
