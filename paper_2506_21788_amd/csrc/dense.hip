@@ -45,39 +45,49 @@ struct DenseArgs {
   int ti, tj;            // tiles
 };
 
-// eight neighbouring values of an operand in float32; n of them exist (the others are zero)
+// Eight neighbouring values of an operand as they come from memory. Nothing is done to them before they are staged: an operation here
+// would wait for the load that is meant to travel while a slice is multiplied.
 template <bool BF, bool MUL>
-__device__ __forceinline__ void load8(const Operand& o, size_t at, int n, float (&v)[8]) {
-  if (n >= 8) {
-    if constexpr (BF) {
-      u32x4_t w;
-      __builtin_memcpy(&w, static_cast<const unsigned short*>(o.p) + at, 16);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        v[2 * k] = __uint_as_float(w[k] << 16);
-        v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
-      }
-    } else {
-      __builtin_memcpy(v, static_cast<const float*>(o.p) + at, 32);
+struct Raw {
+  u32x4_t w[BF ? 1 : 2];
+  u32x4_t m[MUL ? 2 : 1];
+  __device__ __forceinline__ void load(const Operand& o, size_t at) {
+    if constexpr (BF) __builtin_memcpy(&w[0], static_cast<const unsigned short*>(o.p) + at, 16);
+    else __builtin_memcpy(w, static_cast<const float*>(o.p) + at, 32);
+    if constexpr (MUL) __builtin_memcpy(m, o.mul + at, 32);
+  }
+  // n of them exist, the others are zeros
+  __device__ __forceinline__ void load(const Operand& o, size_t at, int n) {
+    if (n >= 8) {
+      load(o, at);
+      return;
     }
-    if constexpr (MUL) {
-      float m[8];
-      __builtin_memcpy(m, o.mul + at, 32);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] *= m[k];
-    }
-  } else {
+    for (int k = 0; k < (BF ? 1 : 2); ++k) w[k] = u32x4_t{0, 0, 0, 0};
+    if constexpr (MUL) m[0] = m[1] = u32x4_t{0, 0, 0, 0};
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      float x = 0.f;
       if (k < n) {
-        if constexpr (BF) x = __uint_as_float((unsigned)static_cast<const unsigned short*>(o.p)[at + k] << 16);
-        else x = static_cast<const float*>(o.p)[at + k];
-        if constexpr (MUL) x *= o.mul[at + k];
+        if constexpr (BF) w[0][k >> 1] |= (unsigned)static_cast<const unsigned short*>(o.p)[at + k] << (16 * (k & 1));
+        else w[k >> 2][k & 3] = __float_as_uint(static_cast<const float*>(o.p)[at + k]);
+        if constexpr (MUL) m[k >> 2][k & 3] = __float_as_uint(o.mul[at + k]);
       }
-      v[k] = x;
     }
   }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if constexpr (BF) v[k] = __uint_as_float(k & 1 ? w[0][k >> 1] & 0xffff0000u : w[0][k >> 1] << 16);
+      else v[k] = __uint_as_float(w[k >> 2][k & 3]);
+      if constexpr (MUL) v[k] *= __uint_as_float(m[k >> 2][k & 3]);
+    }
+  }
+};
+template <bool BF, bool MUL>
+__device__ __forceinline__ void load8(const Operand& o, size_t at, int n, float (&v)[8]) {
+  Raw<BF, MUL> r;
+  r.load(o, at, n);
+  r.values(v);
 }
 
 // eight values as NT bf16 terms
@@ -126,25 +136,56 @@ struct Slice {
     if (KC) { e = c / (BC / 8); k = c % (BC / 8) * 8; }
     else { k = c / (E / 8); e = c % (E / 8) * 8; }
   }
+  // from place e0 of ne along the result and k0 of nk along the contraction. Places past nk are zeros; past ne anything may stand
+  // (their results are not stored). Slices that lie inside take wide loads without a test.
   template <bool BF, bool MUL>
-  __device__ static __forceinline__ void fetch(const Operand& o, int e0, int k0, int ne, int nk, int tid, float (&v)[CH][8]) {
+  __device__ static __forceinline__ void fetch(const Operand& o, int e0, int k0, int ne, int nk, int tid, Raw<BF, MUL> (&v)[CH]) {
+    const bool inside = k0 + BC <= nk && (KC || e0 + E <= ne);   // uniform
+    if (inside) {
 #pragma unroll
-    for (int u = 0; u < CH; ++u) {
-      int e, k;
-      place(tid + u * 256, e, k);
-      e += e0;
-      k += k0;
-      if (KC) load8<BF, MUL>(o, (size_t)(e < ne ? e : 0) * o.ld + (k < nk ? k : 0), e < ne ? nk - k : 0, v[u]);
-      else load8<BF, MUL>(o, (size_t)(k < nk ? k : 0) * o.ld + (e < ne ? e : 0), k < nk ? ne - e : 0, v[u]);
+      for (int u = 0; u < CH; ++u) {
+        int e, k;
+        place(tid + u * 256, e, k);
+        if (KC) v[u].load(o, (size_t)min(e0 + e, ne - 1) * o.ld + k0 + k);
+        else v[u].load(o, (size_t)(k0 + k) * o.ld + e0 + e);
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < CH; ++u) {
+        int e, k;
+        place(tid + u * 256, e, k);
+        e += e0;
+        k += k0;
+        if (KC) v[u].load(o, (size_t)min(e, ne - 1) * o.ld + (k < nk ? k : 0), nk - k);
+        else v[u].load(o, (size_t)(k < nk ? k : 0) * o.ld + (e < ne ? e : 0), k < nk ? ne - e : 0);
+      }
     }
   }
-  __device__ static __forceinline__ void stage(unsigned short* lds, int tid, const float (&v)[CH][8]) {
+  // cs: running sums of the values along the contraction (KC: none)
+  template <bool BF, bool MUL>
+  __device__ static __forceinline__ void stage(unsigned short* lds, int tid, const Raw<BF, MUL> (&v)[CH], float (*cs)[8]) {
 #pragma unroll
     for (int u = 0; u < CH; ++u) {
       int e, k;
       place(tid + u * 256, e, k);
       u32x4_t t[NT];
-      split8<NT>(v[u], t);
+      if constexpr (BF && !MUL && NT == 1) {
+        t[0] = v[u].w[0];
+        if (cs) {
+          float x[8];
+          v[u].values(x);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) cs[u][i] += x[i];
+        }
+      } else {
+        float x[8];
+        v[u].values(x);
+        if (cs) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) cs[u][i] += x[i];
+        }
+        split8<NT>(x, t);
+      }
 #pragma unroll
       for (int q = 0; q < NT; ++q) *reinterpret_cast<u32x4_t*>(lds + q * PLANE + (KC ? e * PITCH + k : k * PITCH + e)) = t[q];
     }
@@ -168,7 +209,7 @@ struct Slice {
 // act(z) and act'(z)
 __device__ __forceinline__ void activate(int act, float z, float& y, float& dy) {
   if (act == HGNN_ACT_SILU) {
-    const float e = __expf(-fabsf(z)), r = 1.0f / (1.0f + e), s = z < 0.f ? e * r : r;   // (no overflow on either side)
+    const float e = __expf(-fabsf(z)), r = __builtin_amdgcn_rcpf(1.0f + e), s = z < 0.f ? e * r : r;   // (no overflow on either side)
     y = z * s;
     dy = s * (1.0f + z * (1.0f - s));
   } else if (act == HGNN_ACT_GELU) {
@@ -232,7 +273,8 @@ __global__ void __launch_bounds__(256) k_dense(DenseArgs a) {
   const int i0 = ti * EI, j0 = tj * EJ;
   const int c0 = split * a.per_split, c1 = min(a.C, c0 + a.per_split);
   f32x16_t acc[WI][WJ] = {};
-  float va[SA::CH][8], vb[SB::CH][8];
+  Raw<BF, AMUL> va[SA::CH];
+  Raw<BF, BMUL> vb[SB::CH];
   float cs[SB::CH][8] = {};
   const bool sums = EPI == EPI_GW && a.colsum && ti == 0;
   if (c0 < c1) {
@@ -241,14 +283,8 @@ __global__ void __launch_bounds__(256) k_dense(DenseArgs a) {
   }
   for (int c = c0; c < c1; c += BC) {
     __syncthreads();
-    SA::stage(la, tid, va);
-    SB::stage(lb, tid, vb);
-    if (sums) {
-#pragma unroll
-      for (int u = 0; u < SB::CH; ++u)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) cs[u][k] += vb[u][k];
-    }
+    SA::template stage<BF, AMUL>(la, tid, va, nullptr);
+    SB::template stage<BF, BMUL>(lb, tid, vb, EPI == EPI_GW && sums ? cs : nullptr);
     if (c + BC < c1) {
       SA::template fetch<BF, AMUL>(a.a, i0, c + BC, a.I, c1, tid, va);
       SB::template fetch<BF, BMUL>(a.b, j0, c + BC, a.J, c1, tid, vb);
