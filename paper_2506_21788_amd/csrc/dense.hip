@@ -14,6 +14,7 @@
 // Small calls (few tiles) take k_dense_small: 32 x 32 results, the contraction dealt to the four wavefronts of a workgroup, operands
 // straight from memory: nothing is staged, the chain is one load, some products and a join.
 #include <climits>
+#include <type_traits>
 
 #include "common.h"
 #include "devmath.h"
@@ -122,11 +123,9 @@ __device__ __forceinline__ bf16x8_t cat(s16x4_t l, s16x4_t h) {
   return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-constexpr int BC = 32;   // contraction places of a slice
-
 // A slice of an operand: E places along the result (E = 64 or 128) by BC along the contraction. KC: its neighbours in memory
 // run along the contraction. NT bf16 terms, one plane each.
-template <int E, bool KC, int NT>
+template <int E, bool KC, int NT, int BC>
 struct Slice {
   static constexpr int PITCH = KC ? BC + 8 : E + 16;          // elements; rows of 16 bytes, in different groups of banks
   static constexpr int PLANE = (KC ? E : BC) * PITCH;
@@ -224,26 +223,69 @@ __device__ __forceinline__ void activate(int act, float z, float& y, float& dy) 
 
 enum { EPI_Y = 0, EPI_GX = 1, EPI_GW = 2 };
 
-// one value of the result
+// four neighbouring values at p[at ..], n of them exist
+__device__ __forceinline__ void put4(float* p, size_t at, const float (&v)[4], int n) {
+  if (n >= 4) {
+    __builtin_memcpy(p + at, v, 16);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < n) p[at + k] = v[k];
+  }
+}
+__device__ __forceinline__ void get4(const float* p, size_t at, float (&v)[4], int n) {
+  if (n >= 4) {
+    __builtin_memcpy(v, p + at, 16);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = k < n ? p[at + k] : 0.f;
+  }
+}
+__device__ __forceinline__ void put4(unsigned short* p, size_t at, const float (&v)[4], int n) {
+  const unsigned w[2] = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+  if (n >= 4) {
+    __builtin_memcpy(p + at, w, 8);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < n) p[at + k] = (unsigned short)(w[k >> 1] >> (16 * (k & 1)));
+  }
+}
+__device__ __forceinline__ void get4(const unsigned short* p, size_t at, float (&v)[4], int n) {
+  unsigned short w[4] = {};
+  if (n >= 4) {
+    __builtin_memcpy(w, p + at, 8);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < n) w[k] = p[at + k];
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = __uint_as_float((unsigned)w[k] << 16);
+}
+
+// Finishes four neighbouring values of row i from column j on, n of them exist. bias, res: theirs (zeros without).
 template <bool BF, int EPI>
-__device__ __forceinline__ void finish(const DenseArgs& a, int i, int j, float v, int split) {
+__device__ __forceinline__ void finish4(const DenseArgs& a, int i, int j, float (&v)[4], int n, int split, const float (&bias)[4], const float (&res)[4]) {
+  using T = typename std::conditional<BF, unsigned short, float>::type;
   const size_t at = (size_t)i * a.J + j;
   if constexpr (EPI == EPI_GW) {
-    a.partial[(size_t)split * a.I * a.J + at] = v;
-    return;
+    put4(a.partial + (size_t)split * a.I * a.J, at, v, n);
+  } else {
+    if constexpr (EPI == EPI_Y) {
+      float d[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float y;
+        activate(a.act, v[k] + bias[k], y, d[k]);
+        v[k] = y;
+      }
+      if (a.dact) put4(a.dact, at, d, n);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] += res[k];
+    put4(static_cast<T*>(a.out), at, v, n);
   }
-  if constexpr (EPI == EPI_Y) {
-    if (a.bias) v += a.bias[j];
-    float y, dy;
-    activate(a.act, v, y, dy);
-    if (a.dact) a.dact[at] = dy;
-    v = y;
-  }
-  if constexpr (EPI != EPI_GW) {
-    if (a.res) v += BF ? __uint_as_float((unsigned)static_cast<const unsigned short*>(a.res)[at] << 16) : static_cast<const float*>(a.res)[at];
-  }
-  if constexpr (BF) static_cast<unsigned short*>(a.out)[at] = (unsigned short)f2bf_bits(v);
-  else static_cast<float*>(a.out)[at] = v;
 }
 
 // tile of a workgroup: the tiles of a row block are neighbours on one XCD (workgroups are dealt to the 8 XCDs in turn), so its
@@ -258,11 +300,15 @@ __device__ __forceinline__ bool tile_of(const DenseArgs& a, int& ti, int& tj, in
   return true;
 }
 
+// contraction places of a slice: as many as leave room for three workgroups a compute unit (fewer barriers and longer loads)
+constexpr int slice_places(int na, int nb) { return na + nb == 2 ? 64 : 32; }
+
 // EI x EJ tile, 2 x 2 wavefronts. AKC / BKC: the operand's neighbours run along the contraction.
 template <bool BF, int EPI, int EI, int EJ, bool AKC, bool BKC, int NA, int NB, bool AMUL, bool BMUL>
-__global__ void __launch_bounds__(256) k_dense(DenseArgs a) {
-  using SA = Slice<EI, AKC, NA>;
-  using SB = Slice<EJ, BKC, NB>;
+__global__ void __launch_bounds__(256, 2) k_dense(DenseArgs a) {
+  constexpr int BC = slice_places(NA, NB);
+  using SA = Slice<EI, AKC, NA, BC>;
+  using SB = Slice<EJ, BKC, NB, BC>;
   extern __shared__ __align__(16) char smem[];
   unsigned short* la = reinterpret_cast<unsigned short*>(smem);
   unsigned short* lb = reinterpret_cast<unsigned short*>(smem + SA::BYTES);
@@ -277,6 +323,11 @@ __global__ void __launch_bounds__(256) k_dense(DenseArgs a) {
   Raw<BF, BMUL> vb[SB::CH];
   float cs[SB::CH][8] = {};
   const bool sums = EPI == EPI_GW && a.colsum && ti == 0;
+  float bias[4] = {};   // of the four columns that this lane finishes
+  if (EPI == EPI_Y && a.bias) {
+    const int q = j0 + wj * (EJ / 2) + lane % (EJ / 8) * 4;
+    if (q < a.J) get4(a.bias, q, bias, a.J - q);
+  }
   if (c0 < c1) {
     SA::template fetch<BF, AMUL>(a.a, i0, c0, a.I, c1, tid, va);
     SB::template fetch<BF, BMUL>(a.b, j0, c0, a.J, c1, tid, vb);
@@ -323,16 +374,54 @@ __global__ void __launch_bounds__(256) k_dense(DenseArgs a) {
       }
     }
   }
+  if constexpr (EPI == EPI_GW) {   // (float32: 32 lanes are a line as they are)
+    float* out = a.partial + (size_t)split * a.I * a.J;
 #pragma unroll
-  for (int i = 0; i < WI; ++i)
+    for (int i = 0; i < WI; ++i)
+#pragma unroll
+      for (int j = 0; j < WJ; ++j)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int r = i0 + wi * (EI / 2) + i * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
+          const int q = j0 + wj * (EJ / 2) + j * 32 + (lane & 31);
+          if (r < a.I && q < a.J) out[(size_t)r * a.J + q] = acc[i][j][v];
+        }
+    return;
+  }
+  // through LDS, 32 rows of a wavefront at a time, so that a lane ends up with four neighbours of a row (always the same columns): a
+  // lane's own sixteen values lie in sixteen rows
+  __syncthreads();
+  using T = typename std::conditional<BF, unsigned short, float>::type;
+  constexpr int COLS = EJ / 2, P = COLS + 4, LPRO = COLS / 4, RP = 64 / LPRO, PASS = 32 / RP;   // lanes of a row, rows of a pass, passes
+  float* sh = reinterpret_cast<float*>(smem) + wave * 32 * P;
+  const int q = j0 + wj * COLS + lane % LPRO * 4, nq = a.J - q;
+#pragma unroll
+  for (int i = 0; i < WI; ++i) {
+    const int r0 = i0 + wi * (EI / 2) + i * 32 + lane / LPRO;
+    auto residual = [&](int u, float (&t)[4]) {
+      if (a.res && r0 + u * RP < a.I && nq > 0) get4(static_cast<const T*>(a.res), (size_t)(r0 + u * RP) * a.J + q, t, nq);
+    };
+    float res[4] = {}, next[4] = {};
+    residual(0, res);
+    if (i) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
 #pragma unroll
     for (int j = 0; j < WJ; ++j)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int r = i0 + wi * (EI / 2) + i * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
-        const int q = j0 + wj * (EJ / 2) + j * 32 + (lane & 31);
-        if (r < a.I && q < a.J) finish<BF, EPI>(a, r, q, acc[i][j][v], split);
-      }
+      for (int v = 0; v < 16; ++v) sh[(8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) * P + j * 32 + (lane & 31)] = acc[i][j][v];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    // (not unrolled: the activations in line 64 times were 54 KB of instructions, run once a workgroup, and took longer than the product)
+#pragma unroll 1
+    for (int u = 0; u < PASS; ++u) {
+      float v[4];
+      *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(sh + (u * RP + lane / LPRO) * P + lane % LPRO * 4);
+      if (u + 1 < PASS) residual(u + 1, next);
+      if (r0 + u * RP < a.I && nq > 0) finish4<BF, EPI>(a, r0 + u * RP, q, v, nq, split, bias, res);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) res[k] = next[k];
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
 }
 
 // 32 x 32 of the result; wavefront w takes contraction places 16 w + 64 t + 0..15
@@ -347,6 +436,11 @@ __global__ void __launch_bounds__(256) k_dense_small(DenseArgs a) {
   const int c0 = split * a.per_split, c1 = min(a.C, c0 + a.per_split);
   f32x16_t acc = {};
   float cs = 0.f;
+  float bias[4] = {};   // of the four columns that this thread finishes
+  if (EPI == EPI_Y && a.bias) {
+    const int q = tj * 32 + (threadIdx.x & 7) * 4;
+    if (q < a.J) get4(a.bias, q, bias, a.J - q);
+  }
   // the lane's eight contraction places c + 0..7 of row e of an operand
   auto get = [&](auto kc, auto mul, const Operand& o, int e, int ne, int c, float (&v)[8]) {
     if constexpr (decltype(kc)::value) {
@@ -393,13 +487,19 @@ __global__ void __launch_bounds__(256) k_dense_small(DenseArgs a) {
       a.colsum[(size_t)split * a.J + j] = s;
     }
   }
-  // the shares are added in the order of the wavefronts; each finishes four rows of every lane
+  // the shares are added in the order of the wavefronts; a thread finishes four neighbours of a row
+  {
+    const int row = threadIdx.x >> 3, col = (threadIdx.x & 7) * 4;
+    const int r = ti * 32 + row, q = tj * 32 + col;
+    if (r < a.I && q < a.J) {
+      const int reg = 4 * (row >> 3) + (row & 3), l0 = 32 * ((row >> 2) & 1) + col;   // of the accumulators
+      float v[4];
 #pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int v = 4 * wave + u;
-    const float s = ((join[0][v][lane] + join[1][v][lane]) + join[2][v][lane]) + join[3][v][lane];
-    const int r = ti * 32 + 8 * wave + 4 * g + u;
-    if (r < a.I && j < a.J) finish<BF, EPI>(a, r, j, s, split);
+      for (int k = 0; k < 4; ++k) v[k] = ((join[0][reg][l0 + k] + join[1][reg][l0 + k]) + join[2][reg][l0 + k]) + join[3][reg][l0 + k];
+      float res[4] = {};
+      if (EPI != EPI_GW && a.res) get4(static_cast<const typename std::conditional<BF, unsigned short, float>::type*>(a.res), (size_t)r * a.J + q, res, a.J - q);
+      finish4<BF, EPI>(a, r, q, v, a.J - q, split, bias, res);
+    }
   }
 }
 
@@ -478,9 +578,10 @@ WSplit weight_split(int64_t M, int64_t K, int64_t N) {
 
 template <bool BF, int EPI, int E, bool AKC, bool BKC, int NA, int NB, bool AMUL, bool BMUL>
 int32_t launch_tile(hipStream_t st, const DenseArgs& a) {
-  const int lds_in = Slice<E, AKC, NA>::BYTES + Slice<E, BKC, NB>::BYTES, lds_cs = EPI == EPI_GW ? 256 * 8 * 4 : 0;
+  constexpr int BC = slice_places(NA, NB);
+  const int lds_in = Slice<E, AKC, NA, BC>::BYTES + Slice<E, BKC, NB, BC>::BYTES, lds_out = EPI == EPI_GW ? 256 * 8 * 4 : 4 * 32 * (E / 2 + 4) * 4;
   const int64_t n = (int64_t)a.ti * a.tj * a.nsplit;
-  k_dense<BF, EPI, E, E, AKC, BKC, NA, NB, AMUL, BMUL><<<(unsigned)((n + 7) / 8 * 8), 256, lds_in > lds_cs ? lds_in : lds_cs, st>>>(a);
+  k_dense<BF, EPI, E, E, AKC, BKC, NA, NB, AMUL, BMUL><<<(unsigned)((n + 7) / 8 * 8), 256, lds_in > lds_out ? lds_in : lds_out, st>>>(a);
   HGNN_LAUNCH_CHECK("k_dense");
   return HGNN_OK;
 }
