@@ -304,7 +304,7 @@ def _own_dense(s):
         return k
 
     k = _buf(s, make)
-    B.dense_fwd(M, K, N, act, dtype, s.x, s.W, s.b, s.r, k.y, k.saved)
+    B.dense_fwd(M, K, N, act, dtype, s.x, s.W, s.b, s.r, k.y, k.saved, k.ws)
     if not c["train"]:
         return {"y": k.y}
     B.dense_bwd(M, K, N, act, dtype, s.x, s.W, k.saved, s.g_y, k.g_x, k.gW, k.g_b, k.ws)
