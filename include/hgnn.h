@@ -432,7 +432,7 @@ int32_t hgnn_graph_attention_bwd(void* stream, int32_t N, int32_t G, int32_t nh,
  * HGNN_F32 products are formed to float32 precision; with HGNN_BF16 x, W, r and y are bfloat16 in memory (hgnn_round_bf16 makes
  * such a copy of a float32 weight buffer, nearest even) and y and g_x are rounded once, g_x from a g_z = g_y act'(z) that is
  * rounded where it enters the product; gW and g_b carry no bf16 rounding.
- * `saved` (NULL: no reverse pass follows) is written by _fwd and read by _bwd; it is empty without an activation.
+ * `saved` (NULL: no reverse pass follows; of the queried size, which may be 0) is written by _fwd and read by _bwd of the same W.
  * _bwd writes g_x = r_x + g_z W^T (r_x NULL: none; g_x NULL: not wanted), gW and g_b (NULL: not wanted); the gradient of r is
  * g_y itself. r_x is what x has as a gradient from elsewhere. y may alias r, g_x may alias r_x.
  * M >= 0, 1 <= K, N <= 8192 (else BAD_SHAPE); M <= 2^26 (else OVERFLOW). Only enqueue work.
@@ -440,7 +440,8 @@ int32_t hgnn_graph_attention_bwd(void* stream, int32_t N, int32_t G, int32_t nh,
 int32_t hgnn_dense_workspace_bytes(int32_t M, int32_t K, int32_t N, int32_t act, int32_t dtype, size_t* ws_bytes_host,
                                    size_t* saved_bytes_host);
 int32_t hgnn_dense_fwd(void* stream, int32_t M, int32_t K, int32_t N, int32_t act, int32_t dtype, const void* x, const void* W,
-                       const float* b, const void* r, void* y /*out*/, void* saved /*or NULL*/, size_t saved_bytes);
+                       const float* b, const void* r, void* y /*out*/, void* saved /*or NULL*/, size_t saved_bytes,
+                       void* ws, size_t ws_bytes);
 int32_t hgnn_dense_bwd(void* stream, int32_t M, int32_t K, int32_t N, int32_t act, int32_t dtype, const void* x, const void* W,
                        const void* saved, size_t saved_bytes, const void* g_y, const void* r_x /*T [M,K] or NULL*/,
                        void* g_x /*out or NULL*/, float* gW /*out [K,N]*/, float* g_b /*out [N] or NULL*/, void* ws, size_t ws_bytes);

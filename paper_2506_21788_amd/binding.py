@@ -315,8 +315,8 @@ def dense_workspace_bytes(M, K, N, act, dtype):
     return a.value, b.value
 
 
-def dense_fwd(M, K, N, act, dtype, x, W, b, r, y, saved):
-    _check(_n.dense_fwd(M, K, N, act, dtype, x, W, b, r, y, saved))
+def dense_fwd(M, K, N, act, dtype, x, W, b, r, y, saved, ws):
+    _check(_n.dense_fwd(M, K, N, act, dtype, x, W, b, r, y, saved, ws))
 
 
 def dense_bwd(M, K, N, act, dtype, x, W, saved, g_y, g_x, gW, g_b, ws, r_x=None):

@@ -139,7 +139,7 @@ class AttentionBlock:
 
     def _dense(self, k, W, b, x, y):
         i, j, act = self.shapes[k]
-        B.dense_fwd(self.N, i, j, act, self.dtype, x, self._m(W), self._p(b), None, y, self.saved[k])
+        B.dense_fwd(self.N, i, j, act, self.dtype, x, self._m(W), self._p(b), None, y, self.saved[k], self.ws)
 
     def _dense_bwd(self, k, W, b, x, g_y, g_x, r_x=None):
         i, j, act = self.shapes[k]

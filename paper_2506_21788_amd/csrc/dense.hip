@@ -11,6 +11,11 @@
 // it stages g_z: no tensor g_z exists. In gW, a sum over all rows, a bf16 call takes g_z as two bf16 terms, as the one
 // rounding that g_z = g_y act'(z) would suffer has no business in a float32 result.
 //
+// The two products with W (large calls): W is laid out once per call in the order in which the matrix cores take it (k_pack), a 1 KB fragment
+// per 32 columns and 16 places, in the one or three bf16 terms, and goes from the L2 to registers without LDS. Staged by every
+// workgroup, half of the LDS traffic and of the splitting was W's, and the LDS was what bound the kernel (128 x 128 x 64:
+// 768 cycles of LDS against 512 of the matrix cores). The forward pass lays out W^T for the reverse pass as well, in `saved`.
+//
 // Small calls (few tiles) take k_dense_small: 32 x 32 results, the contraction dealt to the four wavefronts of a workgroup, operands
 // straight from memory: nothing is staged, the chain is one load, some products and a join.
 #include <climits>
@@ -42,6 +47,8 @@ struct DenseArgs {
   float* dact;           // [I][J] act'(z) or null
   float* partial;        // weight gradient: [nsplit][I][J], then colsum [nsplit][J]
   float* colsum;         // [nsplit][J] column sums of b, or null
+  const u32x4_t* packed; // k_dense_packed: operand b in fragments [term][32 columns][16 places][64 lanes]
+  int pkb, pterm;        // fragments per 32 columns; of a term
   int nsplit, per_split; // contraction slices of a split (multiple of 32 places)
   int ti, tj;            // tiles
 };
@@ -108,14 +115,18 @@ __device__ __forceinline__ void split8(const float (&x)[8], u32x4_t (&o)[NT]) {
   }
 }
 
-// acc += a b over the terms that count, smallest first
-template <int NA, int NB>
-__device__ __forceinline__ f32x16_t mfma_terms(const bf16x8_t (&a)[NA], const bf16x8_t (&b)[NB], f32x16_t acc) {
-  if constexpr (NA == 3 && NB == 3) return mfma_bf16x3(a, b, acc);
-  else {
+// acc[i][j] += a[i] b[j] over the terms that count, smallest first (three terms each: the six products of devmath.h). Term by term
+// over all accumulators: a product that adds to the one before waits for it twice as long as it takes.
+template <int NA, int NB, int WI, int WJ>
+__device__ __forceinline__ void mfma_terms(const bf16x8_t (&a)[WI][NA], const bf16x8_t (&b)[WJ][NB], f32x16_t (&acc)[WI][WJ]) {
+  constexpr int N = NA == 3 ? 6 : NB;
 #pragma unroll
-    for (int t = NB - 1; t >= 0; --t) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b[t], acc, 0, 0, 0);
-    return acc;
+  for (int t = 0; t < N; ++t) {
+    const int ta = NA == 3 ? (t == 0 ? 2 : t == 1 || t == 3 ? 1 : 0) : 0, tb = NA == 3 ? (t == 2 ? 2 : t == 1 || t == 4 ? 1 : 0) : N - 1 - t;
+#pragma unroll
+    for (int i = 0; i < WI; ++i)
+#pragma unroll
+      for (int j = 0; j < WJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i][ta], b[j][tb], acc[i][j], 0, 0, 0);
   }
 }
 
@@ -136,17 +147,18 @@ struct Slice {
     else { k = c / (E / 8); e = c % (E / 8) * 8; }
   }
   // from place e0 of ne along the result and k0 of nk along the contraction. Places past nk are zeros; past ne anything may stand
-  // (their results are not stored). Slices that lie inside take wide loads without a test.
+  // (their results are not stored). Slices that lie inside take wide loads without a test; where neighbours run along the result,
+  // a load past the end of a row reads on in the next one, so only the last of all rows (`all` places) needs the test.
   template <bool BF, bool MUL>
-  __device__ static __forceinline__ void fetch(const Operand& o, int e0, int k0, int ne, int nk, int tid, Raw<BF, MUL> (&v)[CH]) {
-    const bool inside = k0 + BC <= nk && (KC || e0 + E <= ne);   // uniform
+  __device__ static __forceinline__ void fetch(const Operand& o, int e0, int k0, int ne, int nk, int all, int tid, Raw<BF, MUL> (&v)[CH]) {
+    const bool inside = k0 + BC <= nk && (KC || e0 + E <= ne || (k0 + BC < all && ne >= 8));   // uniform
     if (inside) {
 #pragma unroll
       for (int u = 0; u < CH; ++u) {
         int e, k;
         place(tid + u * 256, e, k);
         if (KC) v[u].load(o, (size_t)min(e0 + e, ne - 1) * o.ld + k0 + k);
-        else v[u].load(o, (size_t)(k0 + k) * o.ld + e0 + e);
+        else v[u].load(o, (size_t)(k0 + k) * o.ld + (e0 + e < ne ? e0 + e : 0));
       }
     } else {
 #pragma unroll
@@ -300,6 +312,48 @@ __device__ __forceinline__ bool tile_of(const DenseArgs& a, int& ti, int& tj, in
   return true;
 }
 
+// The results of a workgroup: wavefront (wi, wj) of 2 x 2 has EI / 2 rows and EJ / 2 columns.
+template <bool BF, int EPI, int EI, int EJ>
+__device__ __forceinline__ void store_tile(const DenseArgs& a, const f32x16_t (&acc)[EI / 64][EJ / 64], const float (&bias)[4], int i0, int j0, int wave, int lane,
+                                           char* smem) {
+  constexpr int WI = EI / 64, WJ = EJ / 64;
+  const int wi = wave >> 1, wj = wave & 1;
+  // through LDS, 32 rows of a wavefront at a time, so that a lane ends up with four neighbours of a row (always the same columns): a
+  // lane's own sixteen values lie in sixteen rows
+  __syncthreads();
+  using T = typename std::conditional<BF, unsigned short, float>::type;
+  constexpr int COLS = EJ / 2, P = COLS + 4, LPRO = COLS / 4, RP = 64 / LPRO, PASS = 32 / RP;   // lanes of a row, rows of a pass, passes
+  float* sh = reinterpret_cast<float*>(smem) + wave * 32 * P;
+  const int q = j0 + wj * COLS + lane % LPRO * 4, nq = a.J - q;
+#pragma unroll
+  for (int i = 0; i < WI; ++i) {
+    const int r0 = i0 + wi * (EI / 2) + i * 32 + lane / LPRO;
+    auto residual = [&](int u, float (&t)[4]) {
+      if (a.res && r0 + u * RP < a.I && nq > 0) get4(static_cast<const T*>(a.res), (size_t)(r0 + u * RP) * a.J + q, t, nq);
+    };
+    float res[4] = {}, next[4] = {};
+    residual(0, res);
+    if (i) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+#pragma unroll
+    for (int j = 0; j < WJ; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) sh[(8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) * P + j * 32 + (lane & 31)] = acc[i][j][v];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    // (not unrolled: the activations in line 64 times were 54 KB of instructions, run once a workgroup, and took longer than the product)
+#pragma unroll 1
+    for (int u = 0; u < PASS; ++u) {
+      float v[4];
+      *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(sh + (u * RP + lane / LPRO) * P + lane % LPRO * 4);
+      if (u + 1 < PASS) residual(u + 1, next);
+      if (r0 + u * RP < a.I && nq > 0) finish4<BF, EPI>(a, r0 + u * RP, q, v, nq, 0, bias, res);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) res[k] = next[k];
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 // contraction places of a slice: as many as leave room for three workgroups a compute unit (fewer barriers and longer loads)
 constexpr int slice_places(int na, int nb) { return na + nb == 2 ? 64 : 32; }
 
@@ -329,16 +383,16 @@ __global__ void __launch_bounds__(256, 2) k_dense(DenseArgs a) {
     if (q < a.J) get4(a.bias, q, bias, a.J - q);
   }
   if (c0 < c1) {
-    SA::template fetch<BF, AMUL>(a.a, i0, c0, a.I, c1, tid, va);
-    SB::template fetch<BF, BMUL>(a.b, j0, c0, a.J, c1, tid, vb);
+    SA::template fetch<BF, AMUL>(a.a, i0, c0, a.I, c1, a.C, tid, va);
+    SB::template fetch<BF, BMUL>(a.b, j0, c0, a.J, c1, a.C, tid, vb);
   }
   for (int c = c0; c < c1; c += BC) {
     __syncthreads();
     SA::template stage<BF, AMUL>(la, tid, va, nullptr);
     SB::template stage<BF, BMUL>(lb, tid, vb, EPI == EPI_GW && sums ? cs : nullptr);
     if (c + BC < c1) {
-      SA::template fetch<BF, AMUL>(a.a, i0, c + BC, a.I, c1, tid, va);
-      SB::template fetch<BF, BMUL>(a.b, j0, c + BC, a.J, c1, tid, vb);
+      SA::template fetch<BF, AMUL>(a.a, i0, c + BC, a.I, c1, a.C, tid, va);
+      SB::template fetch<BF, BMUL>(a.b, j0, c + BC, a.J, c1, a.C, tid, vb);
     }
     __syncthreads();
 #pragma unroll
@@ -348,10 +402,7 @@ __global__ void __launch_bounds__(256, 2) k_dense(DenseArgs a) {
       for (int i = 0; i < WI; ++i) SA::read(la, wi * (EI / 2) + i * 32, s, lane, fa[i]);
 #pragma unroll
       for (int j = 0; j < WJ; ++j) SB::read(lb, wj * (EJ / 2) + j * 32, s, lane, fb[j]);
-#pragma unroll
-      for (int i = 0; i < WI; ++i)
-#pragma unroll
-        for (int j = 0; j < WJ; ++j) acc[i][j] = mfma_terms<NA, NB>(fa[i], fb[j], acc[i][j]);
+      mfma_terms<NA, NB, WI, WJ>(fa, fb, acc);
     }
   }
   if constexpr (EPI == EPI_GW) {
@@ -388,40 +439,100 @@ __global__ void __launch_bounds__(256, 2) k_dense(DenseArgs a) {
         }
     return;
   }
-  // through LDS, 32 rows of a wavefront at a time, so that a lane ends up with four neighbours of a row (always the same columns): a
-  // lane's own sixteen values lie in sixteen rows
-  __syncthreads();
-  using T = typename std::conditional<BF, unsigned short, float>::type;
-  constexpr int COLS = EJ / 2, P = COLS + 4, LPRO = COLS / 4, RP = 64 / LPRO, PASS = 32 / RP;   // lanes of a row, rows of a pass, passes
-  float* sh = reinterpret_cast<float*>(smem) + wave * 32 * P;
-  const int q = j0 + wj * COLS + lane % LPRO * 4, nq = a.J - q;
-#pragma unroll
-  for (int i = 0; i < WI; ++i) {
-    const int r0 = i0 + wi * (EI / 2) + i * 32 + lane / LPRO;
-    auto residual = [&](int u, float (&t)[4]) {
-      if (a.res && r0 + u * RP < a.I && nq > 0) get4(static_cast<const T*>(a.res), (size_t)(r0 + u * RP) * a.J + q, t, nq);
-    };
-    float res[4] = {}, next[4] = {};
-    residual(0, res);
-    if (i) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-#pragma unroll
-    for (int j = 0; j < WJ; ++j)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) sh[(8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) * P + j * 32 + (lane & 31)] = acc[i][j][v];
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-    __builtin_amdgcn_wave_barrier();
-    // (not unrolled: the activations in line 64 times were 54 KB of instructions, run once a workgroup, and took longer than the product)
-#pragma unroll 1
-    for (int u = 0; u < PASS; ++u) {
-      float v[4];
-      *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(sh + (u * RP + lane / LPRO) * P + lane % LPRO * 4);
-      if (u + 1 < PASS) residual(u + 1, next);
-      if (r0 + u * RP < a.I && nq > 0) finish4<BF, EPI>(a, r0 + u * RP, q, v, nq, split, bias, res);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) res[k] = next[k];
-    }
-    __builtin_amdgcn_wave_barrier();
+  store_tile<BF, EPI, EI, EJ>(a, acc, bias, i0, j0, wave, lane, smem);
+}
+
+// The result's tile of 128 x 128 where operand b is packed; a: neighbours along the contraction. The slice of a is in LDS twice: one is
+// multiplied while the next is written, a barrier between.
+template <bool BF, int EPI, int NT, bool MUL>
+__global__ void __launch_bounds__(256, 2) k_dense_packed(DenseArgs a) {
+  constexpr int BC = BF ? 64 : 32, KS = BC / 16;
+  using SA = Slice<128, true, NT, BC>;
+  extern __shared__ __align__(16) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wi = wave >> 1, wj = wave & 1;
+  int ti, tj, split;
+  if (!tile_of(a, ti, tj, split)) return;
+  const int i0 = ti * 128, j0 = tj * 128;
+  f32x16_t acc[2][2] = {};
+  Raw<BF, MUL> va[SA::CH];
+  float bias[4] = {};
+  if (EPI == EPI_Y && a.bias) {
+    const int q = j0 + wj * 64 + lane % 16 * 4;
+    if (q < a.J) get4(a.bias, q, bias, a.J - q);
   }
+  const u32x4_t* pb = a.packed + ((size_t)(tj * 4 + wj * 2) * a.pkb) * 64 + lane;
+  bf16x8_t fb[KS][2][NT];
+  auto fetch_b = [&](int c, int s) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) fb[s][j][t] = __builtin_bit_cast(bf16x8_t, pb[((size_t)t * a.pterm + (size_t)j * a.pkb + c / 16 + s) * 64]);
+  };
+  SA::template fetch<BF, MUL>(a.a, i0, 0, a.I, a.C, a.C, tid, va);
+#pragma unroll
+  for (int s = 0; s < KS; ++s) fetch_b(0, s);
+  SA::template stage<BF, MUL>(reinterpret_cast<unsigned short*>(smem), tid, va, nullptr);
+  if (BC < a.C) SA::template fetch<BF, MUL>(a.a, i0, BC, a.I, a.C, a.C, tid, va);
+  __syncthreads();
+  for (int c = 0, at = 0; c < a.C; c += BC, at ^= 1) {
+    const unsigned short* la = reinterpret_cast<const unsigned short*>(smem + at * SA::BYTES);
+    const bool more = c + BC < a.C;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      bf16x8_t fa[2][NT];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+          fa[i][t] = *reinterpret_cast<const bf16x8_t*>(la + t * SA::PLANE + (wi * 64 + i * 32 + (lane & 31)) * SA::PITCH + 16 * s + 8 * (lane >> 5));
+      mfma_terms<NT, NT, 2, 2>(fa, fb[s], acc);
+      if (more) fetch_b(c + BC, s);
+    }
+    if (more) {
+      SA::template stage<BF, MUL>(reinterpret_cast<unsigned short*>(smem + (at ^ 1) * SA::BYTES), tid, va, nullptr);
+      if (c + 2 * BC < a.C) SA::template fetch<BF, MUL>(a.a, i0, c + 2 * BC, a.I, a.C, a.C, tid, va);
+    }
+    __syncthreads();
+  }
+  store_tile<BF, EPI, 128, 128>(a, acc, bias, i0, j0, wave, lane, smem);
+}
+
+// W [K][N] in fragments: lane (n = lane & 31, g) of fragment (32 columns jb, 16 places kb) holds B[16 kb + 8 g + 0..7][32 jb + n], in NT bf16
+// terms; zeros past the edges. First B = W (nf fragments a term), then B = W^T.
+struct PackArgs {
+  const void* W;
+  int K, N;
+  u32x4_t* fwd;
+  int fkb, fterm;   // fragments per 32 columns and of a term; 0: not wanted
+  u32x4_t* bwd;
+  int bkb, bterm;
+};
+template <bool BF>
+__global__ void __launch_bounds__(256) k_pack(PackArgs a) {
+  constexpr int NT = BF ? 1 : 3;
+  long f = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  const bool back = f >= a.fterm;
+  if (back) f -= a.fterm;
+  if (back && f >= a.bterm) return;
+  const int nkb = back ? a.bkb : a.fkb, jb = (int)(f / nkb), kb = (int)(f % nkb);
+  const int c0 = kb * 16 + 8 * (lane >> 5), j = jb * 32 + (lane & 31);   // contraction places and column
+  const int C = back ? a.N : a.K, J = back ? a.K : a.N;
+  const size_t sc = back ? 1 : a.N, sj = back ? a.N : 1;
+  float v[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const bool ok = c0 + k < C && j < J;
+    const size_t at = ok ? (c0 + k) * sc + j * sj : 0;
+    float x;
+    if constexpr (BF) x = __uint_as_float((unsigned)static_cast<const unsigned short*>(a.W)[at] << 16);
+    else x = static_cast<const float*>(a.W)[at];
+    v[k] = ok ? x : 0.f;
+  }
+  u32x4_t o[NT];
+  split8<NT>(v, o);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) (back ? a.bwd : a.fwd)[((size_t)t * (back ? a.bterm : a.fterm) + f) * 64 + lane] = o[t];
 }
 
 // 32 x 32 of the result; wavefront w takes contraction places 16 w + 64 t + 0..15
@@ -434,7 +545,7 @@ __global__ void __launch_bounds__(256) k_dense_small(DenseArgs a) {
   if (!tile_of(a, ti, tj, split)) return;
   const int i = ti * 32 + (lane & 31), j = tj * 32 + (lane & 31);
   const int c0 = split * a.per_split, c1 = min(a.C, c0 + a.per_split);
-  f32x16_t acc = {};
+  f32x16_t acc[1][1] = {};
   float cs = 0.f;
   float bias[4] = {};   // of the four columns that this thread finishes
   if (EPI == EPI_Y && a.bias) {
@@ -465,19 +576,19 @@ __global__ void __launch_bounds__(256) k_dense_small(DenseArgs a) {
     u32x4_t ua[NA], ub[NB];
     split8<NA>(x, ua);
     split8<NB>(y, ub);
-    bf16x8_t fa[NA], fb[NB];
+    bf16x8_t fa[1][NA], fb[1][NB];
 #pragma unroll
-    for (int q = 0; q < NA; ++q) fa[q] = __builtin_bit_cast(bf16x8_t, ua[q]);
+    for (int q = 0; q < NA; ++q) fa[0][q] = __builtin_bit_cast(bf16x8_t, ua[q]);
 #pragma unroll
-    for (int q = 0; q < NB; ++q) fb[q] = __builtin_bit_cast(bf16x8_t, ub[q]);
-    acc = mfma_terms<NA, NB>(fa, fb, acc);
+    for (int q = 0; q < NB; ++q) fb[0][q] = __builtin_bit_cast(bf16x8_t, ub[q]);
+    mfma_terms<NA, NB, 1, 1>(fa, fb, acc);
     if constexpr (EPI == EPI_GW) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) cs += y[k];
     }
   }
 #pragma unroll
-  for (int v = 0; v < 16; ++v) join[wave][v][lane] = acc[v];
+  for (int v = 0; v < 16; ++v) join[wave][v][lane] = acc[0][0][v];
   if constexpr (EPI == EPI_GW) cjoin[wave][lane] = cs;
   __syncthreads();
   if constexpr (EPI == EPI_GW) {
@@ -556,7 +667,8 @@ int tile_size(int64_t I, int64_t J, int64_t splits) {
   return tiles(64) >= cu / 2 ? SIZE_64 : SIZE_32;
 }
 
-// Splits of the weight gradient's contraction (the rows): enough workgroups for two per compute unit, at least 128 rows each.
+// Splits of the weight gradient's contraction (the rows): as many workgroups as run at once, two per compute unit, and no more (7,703 x 866 x
+// 889 float32: 11 splits of 49 tiles, 539 workgroups, took a second turn of them), at least 128 rows each.
 struct WSplit {
   int size, nsplit, per;
 };
@@ -565,7 +677,7 @@ WSplit weight_split(int64_t M, int64_t K, int64_t N) {
   for (int size : {SIZE_128, SIZE_64, SIZE_32}) {
     const int e = size == SIZE_128 ? 128 : size == SIZE_64 ? 64 : 32;
     const int64_t tiles = ((K + e - 1) / e) * ((N + e - 1) / e);
-    const int64_t want = (2 * cu + tiles - 1) / tiles, most = (M + 127) / 128;
+    const int64_t want = 2 * cu / tiles, most = (M + 127) / 128;
     int64_t s = want < most ? want : most;
     if (s < 1) s = 1;
     if (size != SIZE_32 && tiles * s < cu / 2) continue;   // a smaller tile makes more workgroups
@@ -591,7 +703,9 @@ int32_t launch_size(hipStream_t st, DenseArgs a, int size) {
   const int e = size == SIZE_128 ? 128 : size == SIZE_64 ? 64 : 32;
   a.ti = (a.I + e - 1) / e;
   a.tj = (a.J + e - 1) / e;
-  if (size == SIZE_128) return launch_tile<BF, EPI, 128, AKC, BKC, NA, NB, AMUL, BMUL>(st, a);
+  if constexpr (EPI == EPI_GW) {   // (the products with W: k_dense_packed)
+    if (size == SIZE_128) return launch_tile<BF, EPI, 128, AKC, BKC, NA, NB, AMUL, BMUL>(st, a);
+  }
   if (size == SIZE_64) return launch_tile<BF, EPI, 64, AKC, BKC, NA, NB, AMUL, BMUL>(st, a);
   const int64_t n = (int64_t)a.ti * a.tj * a.nsplit;
   k_dense_small<BF, EPI, AKC, BKC, NA, NB, AMUL, BMUL><<<(unsigned)((n + 7) / 8 * 8), 256, 0, st>>>(a);
@@ -608,28 +722,86 @@ int32_t check_dense(int64_t M, int32_t K, int32_t N, int32_t act, int32_t dtype)
   return HGNN_OK;
 }
 
-size_t saved_bytes_of(int64_t M, int N, int act) { return act == HGNN_ACT_NONE ? 0 : (size_t)M * N * sizeof(float); }
-size_t ws_bytes_of(int64_t M, int K, int N) {
+// fragments of a packed operand of C places and J columns: whole slices, whole tiles
+struct Packed {
+  int kb, term;   // fragments per 32 columns, of a term
+  size_t bytes;
+};
+Packed packed_of(int C, int J, bool bf16) {
+  Packed p;
+  p.kb = (C + 63) / 64 * 4;
+  p.term = p.kb * ((J + 127) / 128 * 4);
+  p.bytes = (size_t)p.term * 1024 * (bf16 ? 1 : 3);
+  return p;
+}
+
+// saved: act'(z), then W^T packed for the reverse pass
+struct DenseSaved {
+  float* dact;
+  u32x4_t* wt;
+  size_t bytes;
+};
+DenseSaved carve_saved(void* p, int64_t M, int K, int N, int act, bool bf16) {
+  Carver c(p);
+  DenseSaved s;
+  s.dact = act == HGNN_ACT_NONE ? nullptr : c.take<float>((size_t)M * N);
+  s.wt = tile_size(M, K, 1) == SIZE_128 ? c.take<u32x4_t>(packed_of(N, K, bf16).bytes / 16) : nullptr;
+  s.bytes = c.used();
+  return s;
+}
+// workspace: of the forward pass W packed, of the reverse pass the splits' partials
+size_t fwd_ws_bytes(int64_t M, int K, int N, bool bf16) { return tile_size(M, N, 1) == SIZE_128 ? packed_of(K, N, bf16).bytes : 0; }
+size_t bwd_ws_bytes(int64_t M, int K, int N) {
   if (M == 0) return 0;
   const WSplit w = weight_split(M, K, N);
   return w.nsplit > 1 ? (size_t)w.nsplit * ((size_t)K * N + N) * sizeof(float) : 0;
 }
 
+template <bool BF, int EPI, bool MUL>
+int32_t launch_packed(hipStream_t st, DenseArgs a, const u32x4_t* packed) {
+  constexpr int NT = BF ? 1 : 3, lds_in = 2 * Slice<128, true, NT, BF ? 64 : 32>::BYTES, lds_out = 4 * 32 * (64 + 4) * 4;
+  const Packed p = packed_of(a.C, a.J, BF);
+  a.packed = packed; a.pkb = p.kb; a.pterm = p.term;
+  a.ti = (a.I + 127) / 128;
+  a.tj = (a.J + 127) / 128;
+  const int64_t n = (int64_t)a.ti * a.tj;
+  k_dense_packed<BF, EPI, NT, MUL><<<(unsigned)((n + 7) / 8 * 8), 256, lds_in > lds_out ? lds_in : lds_out, st>>>(a);
+  HGNN_LAUNCH_CHECK("k_dense_packed");
+  return HGNN_OK;
+}
+
 template <bool BF>
-int32_t run_fwd(hipStream_t st, const DenseArgs& a) {
+int32_t run_fwd(hipStream_t st, const DenseArgs& a, const void* W, u32x4_t* packed, u32x4_t* wt) {
+  const bool large = tile_size(a.I, a.J, 1) == SIZE_128;
+  if (large || wt) {
+    PackArgs p{};
+    p.W = W; p.K = a.C; p.N = a.J;
+    if (large) {
+      const Packed f = packed_of(a.C, a.J, BF);
+      p.fwd = packed; p.fkb = f.kb; p.fterm = f.term;
+    }
+    if (wt) {
+      const Packed f = packed_of(a.J, a.C, BF);
+      p.bwd = wt; p.bkb = f.kb; p.bterm = f.term;
+    }
+    k_pack<BF><<<(unsigned)((p.fterm + p.bterm + 3) / 4), 256, 0, st>>>(p);
+    HGNN_LAUNCH_CHECK("k_pack");
+  }
+  if (large) return launch_packed<BF, EPI_Y, false>(st, a, packed);
   return launch_size<BF, EPI_Y, true, false, BF ? 1 : 3, BF ? 1 : 3, false, false>(st, a, tile_size(a.I, a.J, 1));
 }
 
 template <bool BF, bool MUL>
-int32_t run_bwd(hipStream_t st, int M, int K, int N, const void* x, const void* W, const float* dact, const void* g_y, const void* r_x,
-                void* g_x, float* gW, float* g_b, float* ws) {
+int32_t run_bwd(hipStream_t st, int M, int K, int N, const void* x, const void* W, const u32x4_t* wt, const float* dact, const void* g_y,
+                const void* r_x, void* g_x, float* gW, float* g_b, float* ws) {
   if (g_x) {
     DenseArgs a{};
     a.I = M; a.J = K; a.C = N;
     a.a = {g_y, dact, N};
     a.b = {W, nullptr, N};
     a.res = r_x; a.out = g_x; a.nsplit = 1; a.per_split = N;
-    HGNN_TRY((launch_size<BF, EPI_GX, true, true, BF ? 1 : 3, BF ? 1 : 3, MUL, false>(st, a, tile_size(M, K, 1))));
+    if (wt) HGNN_TRY((launch_packed<BF, EPI_GX, MUL>(st, a, wt)));
+    else HGNN_TRY((launch_size<BF, EPI_GX, true, true, BF ? 1 : 3, BF ? 1 : 3, MUL, false>(st, a, tile_size(M, K, 1))));
   }
   const WSplit w = weight_split(M, K, N);
   DenseArgs a{};
@@ -657,28 +829,33 @@ extern "C" int32_t hgnn_dense_workspace_bytes(int32_t M, int32_t K, int32_t N, i
                                               size_t* saved_bytes_host) {
   HGNN_TRY(check_dense(M, K, N, act, dtype));
   HGNN_REQUIRE(ws_bytes_host && saved_bytes_host, HGNN_ERR_NULLPTR, "null size pointer");
-  *ws_bytes_host = ws_bytes_of(M, K, N);
-  *saved_bytes_host = saved_bytes_of(M, N, act);
+  const size_t f = fwd_ws_bytes(M, K, N, dtype == HGNN_BF16), b = bwd_ws_bytes(M, K, N);
+  *ws_bytes_host = f > b ? f : b;
+  *saved_bytes_host = carve_saved(nullptr, M, K, N, act, dtype == HGNN_BF16).bytes;
   return HGNN_OK;
 }
 
 extern "C" int32_t hgnn_dense_fwd(void* stream, int32_t M, int32_t K, int32_t N, int32_t act, int32_t dtype, const void* x, const void* W,
-                                  const float* b, const void* r, void* y, void* saved, size_t saved_bytes) {
+                                  const float* b, const void* r, void* y, void* saved, size_t saved_bytes, void* ws, size_t ws_bytes) {
   HGNN_TRY(check_dense(M, K, N, act, dtype));
   if (M == 0) return HGNN_OK;
   HGNN_REQUIRE(x && W && y, HGNN_ERR_NULLPTR, "dense_fwd: null pointer");
-  const size_t need = saved_bytes_of(M, N, act);
-  HGNN_REQUIRE(!saved || saved_bytes >= need, HGNN_ERR_WORKSPACE_TOO_SMALL, "dense saved buffer: need %zu bytes, got %zu", need, saved_bytes);
+  const DenseSaved s = carve_saved(saved, M, K, N, act, dtype == HGNN_BF16);
+  HGNN_REQUIRE(!saved || saved_bytes >= s.bytes, HGNN_ERR_WORKSPACE_TOO_SMALL, "dense saved buffer: need %zu bytes, got %zu", s.bytes, saved_bytes);
+  const size_t need = fwd_ws_bytes(M, K, N, dtype == HGNN_BF16);
+  HGNN_REQUIRE(need == 0 || ws, HGNN_ERR_NULLPTR, "dense_fwd: null workspace");
+  HGNN_REQUIRE(ws_bytes >= need, HGNN_ERR_WORKSPACE_TOO_SMALL, "dense workspace: need %zu bytes, got %zu", need, ws_bytes);
   DenseArgs a{};
   a.I = M; a.J = N; a.C = K;
   a.a = {x, nullptr, K};
   a.b = {W, nullptr, N};
   a.act = act; a.bias = b; a.res = r; a.out = y;
-  a.dact = act == HGNN_ACT_NONE ? nullptr : static_cast<float*>(saved);
+  a.dact = saved ? s.dact : nullptr;
   a.nsplit = 1; a.per_split = K;
   hipStream_t st = static_cast<hipStream_t>(stream);
+  u32x4_t *pk = static_cast<u32x4_t*>(ws), *wt = saved ? s.wt : nullptr;
   ProfScope ps(PT_MISC, st);
-  return dtype == HGNN_BF16 ? run_fwd<true>(st, a) : run_fwd<false>(st, a);
+  return dtype == HGNN_BF16 ? run_fwd<true>(st, a, W, pk, wt) : run_fwd<false>(st, a, W, pk, wt);
 }
 
 extern "C" int32_t hgnn_dense_bwd(void* stream, int32_t M, int32_t K, int32_t N, int32_t act, int32_t dtype, const void* x, const void* W,
@@ -694,19 +871,19 @@ extern "C" int32_t hgnn_dense_bwd(void* stream, int32_t M, int32_t K, int32_t N,
     return HGNN_OK;
   }
   HGNN_REQUIRE(x && W && g_y, HGNN_ERR_NULLPTR, "dense_bwd: null pointer");
-  HGNN_REQUIRE(act == HGNN_ACT_NONE || saved, HGNN_ERR_NULLPTR, "dense_bwd: an activation needs the saved buffer");
-  const size_t need = saved_bytes_of(M, N, act), wneed = ws_bytes_of(M, K, N);
-  HGNN_REQUIRE(act == HGNN_ACT_NONE || saved_bytes >= need, HGNN_ERR_WORKSPACE_TOO_SMALL, "dense saved buffer: need %zu bytes, got %zu", need, saved_bytes);
+  const DenseSaved s = carve_saved(const_cast<void*>(saved), M, K, N, act, dtype == HGNN_BF16);
+  const size_t wneed = bwd_ws_bytes(M, K, N);
+  HGNN_REQUIRE(s.bytes == 0 || saved, HGNN_ERR_NULLPTR, "dense_bwd: null saved buffer");
+  HGNN_REQUIRE(saved_bytes >= s.bytes || s.bytes == 0, HGNN_ERR_WORKSPACE_TOO_SMALL, "dense saved buffer: need %zu bytes, got %zu", s.bytes, saved_bytes);
   HGNN_REQUIRE(wneed == 0 || ws, HGNN_ERR_NULLPTR, "dense_bwd: null workspace");
   HGNN_REQUIRE(ws_bytes >= wneed, HGNN_ERR_WORKSPACE_TOO_SMALL, "dense workspace: need %zu bytes, got %zu", wneed, ws_bytes);
-  const float* d = static_cast<const float*>(saved);
   float* w = static_cast<float*>(ws);
   ProfScope ps(PT_MISC, st);
   if (dtype == HGNN_BF16)
-    return act == HGNN_ACT_NONE ? run_bwd<true, false>(st, M, K, N, x, W, nullptr, g_y, r_x, g_x, gW, g_b, w)
-                                : run_bwd<true, true>(st, M, K, N, x, W, d, g_y, r_x, g_x, gW, g_b, w);
-  return act == HGNN_ACT_NONE ? run_bwd<false, false>(st, M, K, N, x, W, nullptr, g_y, r_x, g_x, gW, g_b, w)
-                              : run_bwd<false, true>(st, M, K, N, x, W, d, g_y, r_x, g_x, gW, g_b, w);
+    return act == HGNN_ACT_NONE ? run_bwd<true, false>(st, M, K, N, x, W, s.wt, nullptr, g_y, r_x, g_x, gW, g_b, w)
+                                : run_bwd<true, true>(st, M, K, N, x, W, s.wt, s.dact, g_y, r_x, g_x, gW, g_b, w);
+  return act == HGNN_ACT_NONE ? run_bwd<false, false>(st, M, K, N, x, W, s.wt, nullptr, g_y, r_x, g_x, gW, g_b, w)
+                              : run_bwd<false, true>(st, M, K, N, x, W, s.wt, s.dact, g_y, r_x, g_x, gW, g_b, w);
 }
 
 extern "C" int32_t hgnn_round_bf16(void* stream, int64_t n, const float* src, void* dst) {

@@ -94,8 +94,9 @@ def test_dense():
     for kw, code in ((dict(M=-1), SHAPE), (dict(K=0), SHAPE), (dict(N=0), SHAPE), (dict(K=8193), SHAPE), (dict(N=8193), SHAPE), (dict(act=3), SHAPE),
                      (dict(dt=2), SHAPE), (dict(M=(1 << 26) + 1), OVERFLOW)):
         assert size(**kw) == code, kw
-    fwd = lambda x=P, W=P, y=P, s=None, sb=0, M=40: lib.hgnn_dense_fwd(None, i32(M), i32(64), i32(96), i32(1), i32(0), x, W, None, None, y, s, sz(sb))  # noqa: E731
-    for kw, code in ((dict(x=None), NULL), (dict(W=None), NULL), (dict(y=None), NULL), (dict(s=P, sb=8), WS), (dict(M=0, x=None), 0)):
+    fwd = lambda x=P, W=P, y=P, s=None, sb=0, M=40, ws=P, wb=1 << 30: lib.hgnn_dense_fwd(None, i32(M), i32(64), i32(96), i32(1), i32(0), x, W, None, None, y, s, sz(sb), ws, sz(wb))  # noqa: E731
+    for kw, code in ((dict(x=None), NULL), (dict(W=None), NULL), (dict(y=None), NULL), (dict(s=P, sb=8), WS), (dict(M=0, x=None), 0),
+                     (dict(M=40000, ws=None), NULL), (dict(M=40000, wb=8), WS)):
         assert fwd(**kw) == code, kw
 
     def bwd(x=P, W=P, s=P, sb=1 << 30, g=P, gx=P, gW=P, ws=P, wb=1 << 30, M=4000):

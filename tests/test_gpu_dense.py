@@ -24,8 +24,8 @@ def _case(M, K, N, act, dtype, bias=True, res=False, want_gx=True, seed=0, scale
     dx, dW, db, dg = dev(x, dtype), dev(W, dtype), dev(b), dev(g, dtype)
     y, alone, g_x = empty((M, N), dtype), empty((M, N), dtype), empty((M, K), dtype) if want_gx else None
     gW, g_b = empty((K, N)), empty(N) if bias else None
-    B.dense_fwd(M, K, N, ACT[act], code, dx, dW, db, dev(r, dtype), y, saved)
-    B.dense_fwd(M, K, N, ACT[act], code, dx, dW, db, dev(r, dtype), alone, None)
+    B.dense_fwd(M, K, N, ACT[act], code, dx, dW, db, dev(r, dtype), y, saved, ws)
+    B.dense_fwd(M, K, N, ACT[act], code, dx, dW, db, dev(r, dtype), alone, None, ws)
     rx = rounded(rng.standard_normal((M, K)), dtype) if want_gx and res else None
     B.dense_bwd(M, K, N, ACT[act], code, dx, dW, saved, dg, g_x, gW, g_b, ws, r_x=dev(rx, dtype))
     torch.cuda.synchronize()
@@ -82,7 +82,7 @@ def test_far_arguments_of_the_activations(act):
     one = torch.eye(n, device="cuda")
     ws_b, saved_b = B.dense_workspace_bytes(1, n, n, ACT[act], B.F32)
     saved, y, g_x, gW = torch.empty(saved_b, dtype=torch.uint8, device="cuda"), empty((1, n)), empty((1, n)), empty((n, n))
-    B.dense_fwd(1, n, n, ACT[act], B.F32, z, one, None, None, y, saved)
+    B.dense_fwd(1, n, n, ACT[act], B.F32, z, one, None, None, y, saved, None)
     B.dense_bwd(1, n, n, ACT[act], B.F32, z, one, saved, torch.ones((1, n), device="cuda"), g_x, gW, None, torch.empty(max(ws_b, 16), dtype=torch.uint8, device="cuda"))
     a, d = ob.activation(z.double().cpu().numpy(), act)
     assert np.allclose(y.cpu().numpy(), a, rtol=1e-5, atol=1e-7) and np.allclose(g_x.cpu().numpy(), d, rtol=1e-5, atol=1e-6)
@@ -94,13 +94,13 @@ def test_no_rows_and_in_place_residual(dtype):
     from paper_2506_21788_amd import binding as B
     code = B.BF16 if dtype == "bf16" else B.F32
     gW, g_b, none = empty((5, 7)), empty(7), empty((0, 5), dtype)
-    B.dense_fwd(0, 5, 7, 1, code, none, none, None, None, none, None)
+    B.dense_fwd(0, 5, 7, 1, code, none, none, None, None, none, None, None)
     B.dense_bwd(0, 5, 7, 1, code, none, none, None, none, none, gW, g_b, None)
     assert torch.equal(gW, torch.zeros_like(gW)) and torch.equal(g_b, torch.zeros_like(g_b))
     x, W, r = (dev(np.random.default_rng(k).standard_normal((70, 70)), dtype) for k in range(3))
     y = empty((70, 70), dtype)
-    B.dense_fwd(70, 70, 70, 1, code, x, W, None, r, y, None)
-    B.dense_fwd(70, 70, 70, 1, code, x, W, None, r, r, None)
+    B.dense_fwd(70, 70, 70, 1, code, x, W, None, r, y, None, None)
+    B.dense_fwd(70, 70, 70, 1, code, x, W, None, r, r, None, None)
     assert torch.equal(y, r)
 
 
@@ -129,7 +129,7 @@ def test_in_a_graph_on_another_stream():
     out = [empty((M, N), "bf16"), empty((M, K), "bf16"), empty((K, N)), empty(N)]
 
     def both():
-        B.dense_fwd(M, K, N, 1, B.BF16, x, W, b, None, out[0], saved)
+        B.dense_fwd(M, K, N, 1, B.BF16, x, W, b, None, out[0], saved, ws)
         B.dense_bwd(M, K, N, 1, B.BF16, x, W, saved, g, out[1], out[2], out[3], ws)
 
     both()
