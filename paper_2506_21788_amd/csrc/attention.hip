@@ -215,20 +215,28 @@ struct Weights<true> {
     }
   }
 };
-// what is left of them after that rounding
-__device__ __forceinline__ Weights<true> remainder_of(const f32x16_t& p, const Weights<true>& w) {
-  f32x16_t r;
+// the same as three terms that add up to the weights exactly: the high 16 bits, those of the remainder, and what is left (8 bits)
+struct Weights3 {
+  bf16x8_t w[3][2];
+  __device__ __forceinline__ explicit Weights3(const f32x16_t& p) {
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const u32x4_t u = __builtin_bit_cast(u32x4_t, w.w[t]);
+    for (int t = 0; t < 2; ++t) {
+      u32x4_t u[3];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      r[8 * t + 2 * k] = p[8 * t + 2 * k] - __uint_as_float(u[k] << 16);
-      r[8 * t + 2 * k + 1] = p[8 * t + 2 * k + 1] - __uint_as_float(u[k] & 0xffff0000u);
+      for (int k = 0; k < 4; ++k) {
+        float x = p[8 * t + 2 * k], y = p[8 * t + 2 * k + 1];
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+          u[q][k] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+          x -= __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+          y -= __uint_as_float(__float_as_uint(y) & 0xffff0000u);
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < 3; ++q) w[q][t] = __builtin_bit_cast(bf16x8_t, u[q]);
     }
   }
-  return Weights<true>(r);
-}
+};
 template <>
 struct Weights<false> {
   f32x16_t w;
@@ -252,16 +260,16 @@ __device__ __forceinline__ void add_cols(const typename Row<BF, DP>::T* tile, co
     }
   }
 }
-// the same with weights of two bf16 terms
+// the same with weights of three bf16 terms, smallest first
 template <int DP>
-__device__ __forceinline__ void add_cols2(const unsigned short* tile, const Weights<true>& w, const Weights<true>& w2, f32x16_t (&acc)[DP / 32], int lane) {
+__device__ __forceinline__ void add_cols3(const unsigned short* tile, const Weights3& w, f32x16_t (&acc)[DP / 32], int lane) {
 #pragma unroll
   for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const bf16x8_t c = read_col(tile, Row<true, DP>::PITCH, b, t, lane);
-      acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c, w2.w[t], acc[b], 0, 0, 0);
-      acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c, w.w[t], acc[b], 0, 0, 0);
+#pragma unroll
+      for (int q = 2; q >= 0; --q) acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c, w.w[q][t], acc[b], 0, 0, 0);
     }
 }
 // the same where both operands are tiles in LDS: acc[b][d][col] += sum over rows of tile[row][32 b + d] w[row][col]
@@ -440,35 +448,40 @@ __device__ __forceinline__ Where tile_where(const AttnArgs& a, int t) {
   return w;
 }
 
-// LDS: the tables first, then each wavefront's tiles, then (SPLIT) room for the join
+// LDS: the tables first, then each wavefront's tiles (and over them, when they have been used, its share of a join)
 template <bool BF, int DP>
 constexpr int tile_bytes() { return 32 * Row<BF, DP>::PITCH * (BF ? 2 : 4); }
-constexpr int join_bytes(int DP) { return DP * 32 * 4 + 512; }
-constexpr int FWD_TABLE = 1024, DQ_TABLE = 2048;   // entries of 4 bytes; of 8: bias and place in the sums of g_bias
+constexpr int TABLE = 1024;
 template <bool BF, int DP>
-__host__ __device__ constexpr int dq_wave_bytes(int nb) { return 2 * tile_bytes<BF, DP>() + (nb + 1) * 256; }
+__host__ __device__ constexpr int fwd_wave_bytes() { return 2 * tile_bytes<BF, DP>() + 256; }
+template <bool BF, int DP, int COLS>
+__host__ __device__ constexpr int dq_wave_bytes(int nb) { return 2 * tile_bytes<BF, DP>() + (nb + 1) * COLS * 4; }
 template <bool BF, int DP>
 constexpr int dkv_wave_bytes() { return 2 * tile_bytes<BF, DP>() + 2 * tile_bytes<BF, 32>(); }
 
-// x of the wavefronts of a workgroup, added in order: the sum is wavefront 0's
+// x of the wavefronts of a workgroup, added in order: the sum is wavefront 0's. room: that of wavefront 0; the others' are `stride`
+// bytes on. The barriers around it keep what lies there before and after.
 template <int NB>
-__device__ __forceinline__ void join_sum(f32x16_t (&x)[NB], float* room, int nw, int wave, int lane) {
-  for (int k = 1; k < nw; ++k) {
-    __syncthreads();
-    if (wave == k) {
+__device__ __forceinline__ void join_sum(f32x16_t (&x)[NB], char* room, int stride, int nw, int wave, int lane) {
+  __syncthreads();
+  if (wave) {
+    float* mine = reinterpret_cast<float*>(room + wave * stride);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mine[(b * 16 + i) * 64 + lane] = x[b][i];
+  }
+  __syncthreads();
+  if (wave == 0) {
+    for (int k = 1; k < nw; ++k) {
+      const float* theirs = reinterpret_cast<const float*>(room + k * stride);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) room[(b * 16 + i) * 64 + lane] = x[b][i];
-    }
-    __syncthreads();
-    if (wave == 0) {
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[b][i] += room[(b * 16 + i) * 64 + lane];
+        for (int i = 0; i < 16; ++i) x[b][i] += theirs[(b * 16 + i) * 64 + lane];
     }
   }
+  __syncthreads();
 }
 
 // -------------------------------------------------------------------------------------------------------------------------
@@ -483,7 +496,7 @@ __global__ void __launch_bounds__(256, DP == 128 ? 1 : 2) k_attn_fwd(AttnArgs a)
   if (t >= ntiles) return;   // uniform over the workgroup
   const Where w = tile_where(a, t);
   float* table = reinterpret_cast<float*>(smem);
-  T* tk = reinterpret_cast<T*>(smem + FWD_TABLE + wave * 2 * tile_bytes<BF, DP>());
+  T* tk = reinterpret_cast<T*>(smem + TABLE + wave * fwd_wave_bytes<BF, DP>());
   T* tv = tk + 32 * Row<BF, DP>::PITCH;
   fill_table(table, a.bias + (size_t)h * a.nb, a.nb, a.inv, lane);   // (SPLIT: the same values by every wavefront)
   lds_order();
@@ -540,41 +553,39 @@ __global__ void __launch_bounds__(256, DP == 128 ? 1 : 2) k_attn_fwd(AttnArgs a)
 #pragma unroll
     for (int i = 4; i < 16; ++i) l4[i & 3] += s[i];
     l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
-    const Weights<BF> p(s);
-    // bf16: the weights enter as two terms. The reverse pass takes D from the output, and one rounding of the weights (2^-9) there
-    // is more than the bias gradient, a sum of differences, can bear; two more products and 40 operations of some 200 a tile
-    if constexpr (BF) add_cols2<DP>(tv, p, remainder_of(s, p), o, lane);
-    else add_cols<BF, DP>(tv, p, o, lane);
+    // bf16: the weights enter as they are, as three terms. The reverse pass takes D from the output, and a rounding of the weights
+    // there is more than the bias gradient, a sum of differences over all pairs, can bear (two terms: off by 1e-6 to 7e-6 where
+    // float32 is off by 1e-7 to 2e-6)
+    if constexpr (BF) add_cols3<DP>(tv, Weights3(s), o, lane);
+    else add_cols<BF, DP>(tv, Weights<BF>(s), o, lane);
   }
   l += other_half(l);
 
   if constexpr (SPLIT) {   // the wavefronts' shares, in order
-    char* join = smem + FWD_TABLE + a.nw * 2 * tile_bytes<BF, DP>();
-    float* jo = reinterpret_cast<float*>(join);
-    float* jm = reinterpret_cast<float*>(join + DP * 32 * 4);
-    for (int k2 = 1; k2 < a.nw; ++k2) {
-      __syncthreads();
-      if (wave == k2) {
+    constexpr int WB = fwd_wave_bytes<BF, DP>();
+    __syncthreads();
+    if (wave) {
+      float* mine = reinterpret_cast<float*>(smem + TABLE + wave * WB);
 #pragma unroll
-        for (int b = 0; b < DP / 32; ++b)
+      for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) jo[(b * 16 + i) * 64 + lane] = o[b][i];
-        if (lane < 32) { jm[lane] = m; jm[32 + lane] = l; }
-      }
-      __syncthreads();
-      if (wave == 0) {   // (a sum that is no number stays one)
-        const float m2 = jm[lane & 31], l2 = jm[32 + (lane & 31)], mn = fmaxf(m, m2);
-        const float f1 = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m - mn) * a.c);
-        const float f2 = m2 == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m2 - mn) * a.c);
-        l = l * f1 + l2 * f2;
-        m = mn;
-#pragma unroll
-        for (int b = 0; b < DP / 32; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[b][i] = o[b][i] * f1 + jo[(b * 16 + i) * 64 + lane] * f2;
-      }
+        for (int i = 0; i < 16; ++i) mine[(b * 16 + i) * 64 + lane] = o[b][i];
+      if (lane < 32) { mine[DP * 32 + lane] = m; mine[DP * 32 + 32 + lane] = l; }
     }
+    __syncthreads();
     if (wave) return;
+    for (int k2 = 1; k2 < a.nw; ++k2) {   // (a sum that is no number stays one)
+      const float* jo = reinterpret_cast<const float*>(smem + TABLE + k2 * WB);
+      const float m2 = jo[DP * 32 + (lane & 31)], l2 = jo[DP * 32 + 32 + (lane & 31)], mn = fmaxf(m, m2);
+      const float f1 = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m - mn) * a.c);
+      const float f2 = m2 == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m2 - mn) * a.c);
+      l = l * f1 + l2 * f2;
+      m = mn;
+#pragma unroll
+      for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] = o[b][i] * f1 + jo[(b * 16 + i) * 64 + lane] * f2;
+    }
   }
 
   const size_t orow = ((size_t)w.lo + qi) * a.nh + h;   // row of out
@@ -624,57 +635,69 @@ __global__ void __launch_bounds__(256, DP == 128 ? 1 : 2) k_attn_fwd(AttnArgs a)
   }
 }
 
-// sum of a bucket's 64 columns (a lane per bucket: the columns are taken in turn, from its own on, so that no bank is hit twice)
-__device__ __forceinline__ float hist_sum(const float* hist, int b) {
+// The sums of g_bias of a wavefront: COLS words of LDS per bucket, and as many more for the pairs that are left out. 64: a column per
+// lane. 32, in long graphs: lanes i and i + 32 share one and take turns, and twice as many wavefronts fit a compute unit.
+template <int COLS>
+__device__ __forceinline__ float hist_sum(const float* hist, int b) {   // (a lane per bucket: the columns from its own on, so that no bank is hit twice)
   float s[8] = {};
 #pragma unroll
-  for (int k = 0; k < 64; ++k) s[k & 7] += hist[b * 64 + ((k + b) & 63)];
+  for (int k = 0; k < COLS; ++k) s[k & 7] += hist[b * COLS + ((k + b) & (COLS - 1))];
   return ((s[0] + s[4]) + (s[1] + s[5])) + ((s[2] + s[6]) + (s[3] + s[7]));
 }
 
-// Adds to this lane's words of LDS, HB at a time: they are read together, and one that is named twice takes up what the earlier
-// one has made of it. (Adding in LDS itself, ds_add_f32, took 210 cycles of the compute unit for 64 words.)
+// Adds to this lane's words, HB at a time: they are read together, and one that is named twice takes up what the earlier one has
+// made of it. (Adding in LDS itself, ds_add_f32, took 210 cycles of the compute unit for 64 words; four at a time, with six
+// comparisons, were slower than two.)
 constexpr int HB = 2;
-__device__ __forceinline__ void hist_read(const unsigned (&at)[16], int i, float (&v)[HB]) {
+template <int COLS>
+__device__ __forceinline__ void hist_at(const u32x4_t& bk, int i, int nb, unsigned col, unsigned (&at)[HB]) {
 #pragma unroll
-  for (int k = 0; k < HB; ++k) v[k] = lds<float>(at[i + k]);
+  for (int k = 0; k < HB; ++k) at[k] = min(entry_of<COLS == 64 ? 8 : 7>(bk, i + k), (unsigned)nb * (COLS * 4)) + col;
 }
-__device__ __forceinline__ void hist_add(const unsigned (&at)[16], int i, float (&v)[HB], const f32x16_t& x) {
+__device__ __forceinline__ void hist_read(const unsigned (&at)[HB], float (&v)[HB]) {
+#pragma unroll
+  for (int k = 0; k < HB; ++k) v[k] = lds<float>(at[k]);
+}
+__device__ __forceinline__ void hist_add(const unsigned (&at)[HB], float (&v)[HB], const f32x16_t& x, int i) {
 #pragma unroll
   for (int k = 0; k < HB; ++k) {
 #pragma unroll
-    for (int u = 0; u < k; ++u) v[k] = at[i + k] == at[i + u] ? v[u] : v[k];
+    for (int u = 0; u < k; ++u) v[k] = at[k] == at[u] ? v[u] : v[k];
     v[k] += x[i + k];
   }
 #pragma unroll
-  for (int k = 0; k < HB; ++k) lds<float>(at[i + k]) = v[k];
+  for (int k = 0; k < HB; ++k) lds<float>(at[k]) = v[k];
+}
+// bytes of w that differ from those of v
+__device__ __forceinline__ int bytes_unlike(unsigned w, unsigned v) {
+  const unsigned t = w ^ v;
+  return __popc((((t & 0x7f7f7f7fu) + 0x7f7f7f7fu) | t) & 0x80808080u);
 }
 
 // -------------------------------------------------------------------------------------------------------------------------
 // g_q of 32 queries, D of theirs, and g_bias. A workgroup of head h takes tiles me, me + per_head, ...
-template <bool BF, int DP, bool SPLIT>
-__global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k_attn_dq(AttnArgs a) {
+// LONG (graphs of 1,024 atoms and more, SPLIT): nearly all pairs of most tiles are in the last bucket. Those are added up in a register,
+// the few others one by one in LDS, where an addition takes some three cycles a lane that takes part.
+template <bool BF, int DP, bool SPLIT, bool LONG>
+__global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : BF && DP == 32 ? 3 : 2) k_attn_dq(AttnArgs a) {
   using T = typename Row<BF, DP>::T;
+  constexpr int COLS = LONG ? 32 : 64;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x & 63, wave = SPLIT ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0, g = lane >> 5;
   int me, h;
   item_of(a.near, blockIdx.x, a.nh, me, h);
   if (me >= a.per_head) return;   // uniform over the workgroup
-  const int wave_bytes = dq_wave_bytes<BF, DP>(a.nb);
-  float2* table = reinterpret_cast<float2*>(smem);
-  T* tk = reinterpret_cast<T*>(smem + DQ_TABLE + wave * wave_bytes);
+  const int wave_bytes = dq_wave_bytes<BF, DP, COLS>(a.nb);
+  float* table = reinterpret_cast<float*>(smem);
+  T* tk = reinterpret_cast<T*>(smem + TABLE + wave * wave_bytes);
   T* tv = tk + 32 * Row<BF, DP>::PITCH;
-  const unsigned hist_at = DQ_TABLE + wave * wave_bytes + 2 * tile_bytes<BF, DP>();
-  float* hist = reinterpret_cast<float*>(smem + hist_at);
-  // a bucket's bias and the place of its column; what is left out, by its byte or a bias of -inf, has a column of its own
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const float v = table_value(a.bias + (size_t)h * a.nb, a.nb, k * 64 + lane, a.inv);
-    table[k * 64 + lane] = make_float2(v, __uint_as_float((v > -__builtin_inff() ? k * 64 + lane : a.nb) * 256u));
-  }
-  for (int b = 0; b <= a.nb; ++b) hist[b * 64 + lane] = 0.f;
+  const unsigned hist0 = TABLE + wave * wave_bytes + 2 * tile_bytes<BF, DP>();
+  float* hist = reinterpret_cast<float*>(smem + hist0);
+  fill_table(table, a.bias + (size_t)h * a.nb, a.nb, a.inv, lane);
+  for (int b = lane; b < (a.nb + 1) * COLS; b += 64) hist[b] = 0.f;
   lds_order();
-  const unsigned my_col = hist_at + lane * 4;
+  const unsigned col = hist0 + (lane & (COLS - 1)) * 4;
+  float far_sum = 0.f;
   const int hk = h / (a.nh / a.nkv);
   const unsigned ld = (unsigned)(a.nh + 2 * a.nkv) * a.dh, lo_ = (unsigned)a.nh * a.dh;
   const int ntiles = *a.plan.count;
@@ -714,13 +737,14 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k
       lds_order();
       kt.to_lds(tk, lane);
       vt.to_lds(tv, lane);
-      f32x16_t s;
-      unsigned at[16];
+      f32x16_t s = biases(0, bk);
+      const u32x4_t bc = bk;
+      bool far = false;
+      if constexpr (LONG) {
+        int others = 0;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const f32x2v_t e = lds<const f32x2v_t>(entry_of<3>(bk, i));
-        s[i] = e[0];
-        at[i] = __float_as_uint(e[1]) + my_col;
+        for (int i = 0; i < 4; ++i) others += bytes_unlike(bc[i], (a.nb - 1) * 0x01010101u);
+        far = !__any(others > 3);
       }
       lds_order();
       if (j0 + step < w.n) fetch(j0 + step);
@@ -728,21 +752,55 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k
       s = Row<BF, DP>::dot(k, q, s);
       v.from_lds(tv, tile_row(lane & 31), g);
       f32x16_t ds = Row<BF, DP>::dot(v, go, f32x16_t{});
-      // (the first words of the sums of g_bias are on their way while the weights are formed, the next while the ones before are added)
-      float v4[HB];
-      hist_read(at, 0, v4);
+      unsigned at[HB];
+      float h2[HB];
+      if (!LONG) {   // (the first words of the sums are on their way while the weights are formed, the next while the ones before are added)
+        hist_at<COLS>(bc, 0, a.nb, col, at);
+        hist_read(at, h2);
+      }
       weights_of(s, a.c, st.x, st.y);
 #pragma unroll
-      for (int i = 0; i < 16; i += HB) {
+      for (int i = 0; i < 16; ++i) {
+        ds[i] = s[i] * (ds[i] - D);
+        if (!LONG && i % HB == HB - 1) {
+          hist_add(at, h2, ds, i - (HB - 1));
+          if (i < 15) {
+            hist_at<COLS>(bc, i + 1, a.nb, col, at);
+            hist_read(at, h2);
+          }
+        }
+      }
+      if constexpr (LONG) {
+        const unsigned last = (a.nb - 1) * 128u;
+        if (far) {
 #pragma unroll
-        for (int u = 0; u < HB; ++u) ds[i + u] = s[i + u] * (ds[i + u] - D);
-        hist_add(at, i, v4, ds);
-        if (i + HB < 16) hist_read(at, i + HB, v4);
+          for (int i = 0; i < 16; ++i) {
+            const unsigned e = entry_of<7>(bc, i);
+            far_sum += e == last ? ds[i] : 0.f;
+            if (__any(e < last)) {   // (the two lanes of a column, one after the other)
+              if (e < last && g == 0) __hip_atomic_fetch_add(&lds<float>(e + col), ds[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+              if (e < last && g == 1) __hip_atomic_fetch_add(&lds<float>(e + col), ds[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            }
+          }
+        } else {
+          for (int half = 0; half < 2; ++half) {
+            if (g == half) {
+#pragma unroll
+              for (int i = 0; i < 16; i += HB) {
+                hist_at<COLS>(bc, i, a.nb, col, at);
+                hist_read(at, h2);
+                hist_add(at, h2, ds, i);
+              }
+            }
+            lds_order();
+          }
+        }
       }
       add_cols<BF, DP>(tk, Weights<BF>(ds), dq, lane);
     }
     if constexpr (SPLIT) {
-      join_sum<DP / 32>(dq, reinterpret_cast<float*>(smem + DQ_TABLE + a.nw * wave_bytes), a.nw, wave, lane);
+      static_assert(DP * 128 <= 2 * tile_bytes<BF, DP>(), "room for the join");
+      join_sum<DP / 32>(dq, smem + TABLE, wave_bytes, a.nw, wave, lane);
       if (wave) continue;
     }
     T* gq = static_cast<T*>(a.g_qkv) + (size_t)w.lo * ld + (size_t)h * a.dh;
@@ -767,7 +825,7 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k
       const uint8_t* row = w.pairs + (w.i0 + r) * w.pitch;
       float a0 = 0.f, a1 = 0.f;
       for (int j = 0; j < w.n; ++j) {
-        const float b = table[row[j]].x;
+        const float b = table[row[j]];
         if (b == -__builtin_inff()) continue;
         const size_t kj = ((size_t)w.lo + j) * ld + (size_t)(a.nh + hk) * a.dh, vj = kj + (size_t)a.nkv * a.dh;
         const float k0 = d0 ? value<BF>(a.qkv, kj + lane) : 0.f, k1 = d1 ? value<BF>(a.qkv, kj + lane + 64) : 0.f;
@@ -782,12 +840,16 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k
     }
   }
 
+  if constexpr (LONG) {
+    far_sum += other_half(far_sum);
+    if (g == 0) lds<float>((a.nb - 1) * 128u + col) += far_sum;
+  }
   lds_order();
   if constexpr (SPLIT) __syncthreads();
   if (wave == 0 && lane < a.nb) {
     float s = 0.f;
     for (int k2 = 0; k2 < (SPLIT ? a.nw : 1); ++k2)
-      s += hist_sum(reinterpret_cast<const float*>(smem + DQ_TABLE + k2 * wave_bytes + 2 * tile_bytes<BF, DP>()), lane);
+      s += hist_sum<COLS>(reinterpret_cast<const float*>(smem + hist0 + k2 * wave_bytes), lane);
     a.partial[((size_t)h * a.per_head + me) * a.nb + lane] = s;
   }
 }
@@ -811,6 +873,7 @@ __device__ __forceinline__ void bias_reduce(const AttnArgs& a, int h, float* sh)
   __syncthreads();
   if (run == 0 && b < a.nb) {
     for (int k = 1; k < runs; ++k) s += sh[k * 64 + b];
+    if (a.bias[(size_t)h * a.nb + b] == -__builtin_inff()) s = 0.f;   // its pairs are left out
     a.g_bias[(size_t)h * a.nb + b] = s;
   }
 }
@@ -834,9 +897,9 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k
   if (t >= ntiles) return;
   const Where w = tile_where(a, t);
   // (tables: wavefronts of one workgroup may be at different heads, so each has its own)
-  const unsigned table_at = wave * FWD_TABLE;
+  const unsigned table_at = wave * TABLE;
   float* table = reinterpret_cast<float*>(smem + table_at);
-  T* tq = reinterpret_cast<T*>(smem + (SPLIT ? a.nw : 1) * FWD_TABLE + wave * dkv_wave_bytes<BF, DP>());
+  T* tq = reinterpret_cast<T*>(smem + (SPLIT ? a.nw : 1) * TABLE + wave * dkv_wave_bytes<BF, DP>());
   T* tg = tq + 32 * Row<BF, DP>::PITCH;
   T* tp = tg + 32 * Row<BF, DP>::PITCH;
   T* ts = tp + 32 * PT;
@@ -900,9 +963,9 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k
     }
   }
   if constexpr (SPLIT) {
-    float* room = reinterpret_cast<float*>(smem + a.nw * (FWD_TABLE + dkv_wave_bytes<BF, DP>()));
-    join_sum<DP / 32>(dk, room, a.nw, wave, lane);
-    join_sum<DP / 32>(dv, room, a.nw, wave, lane);
+    char* room = smem + a.nw * TABLE;
+    join_sum<DP / 32>(dk, room, dkv_wave_bytes<BF, DP>(), a.nw, wave, lane);
+    join_sum<DP / 32>(dv, room, dkv_wave_bytes<BF, DP>(), a.nw, wave, lane);
     if (wave) return;
   }
   const int kj = w.i0 + (lane & 31);
@@ -1012,35 +1075,34 @@ int32_t check_attn(int32_t N, int32_t G, int32_t nh, int32_t nkv, int32_t dh, in
 // wavefronts of 625 tiles each leave a fifth of the SIMDs idle at the end; four times as many of a quarter the length do not, and
 // the join is small against their chains.
 // Where keys are shared by query heads, k_attn_dkv has few and long chains as well.
+bool long_graphs(int64_t G, int64_t N) { return N >= 1024 * G; }
 bool attn_split(int64_t max_tiles, int heads, int64_t G, int64_t N, int rep) {
-  return (max_tiles * heads <= 4 * num_cus() && N * rep > 2 * PAIR_T * G) || N >= 1024 * G || rep > 1;
+  return (max_tiles * heads <= 4 * num_cus() && N * rep > 2 * PAIR_T * G) || long_graphs(G, N) || rep > 1;
 }
 
 template <bool BF, int DP, bool SPLIT>
 int32_t launch_fwd(hipStream_t st, AttnArgs a) {
-  const int extra = FWD_TABLE + (SPLIT ? join_bytes(DP) : 0);
-  constexpr int WB = 2 * tile_bytes<BF, DP>();
+  constexpr int WB = fwd_wave_bytes<BF, DP>(), extra = TABLE;
   a.nw = SPLIT ? waves_that_fit(WB, extra) : 1;
   k_attn_fwd<BF, DP, SPLIT><<<(unsigned)item_blocks(a.near, a.plan.max_tiles, a.nh), 64 * a.nw, WB * a.nw + extra, st>>>(a);
   HGNN_LAUNCH_CHECK("k_attn_fwd");
   return HGNN_OK;
 }
 
-template <bool BF, int DP, bool SPLIT>
+template <bool BF, int DP, bool SPLIT, bool LONG>
 int32_t launch_dq(hipStream_t st, AttnArgs a) {
-  const int wb = dq_wave_bytes<BF, DP>(a.nb), extra = DQ_TABLE + (SPLIT ? join_bytes(DP) : 0);
+  const int wb = dq_wave_bytes<BF, DP, LONG ? 32 : 64>(a.nb), extra = TABLE;
   a.nw = SPLIT ? waves_that_fit(wb, extra) : 1;
-  k_attn_dq<BF, DP, SPLIT><<<(unsigned)item_blocks(a.near, a.per_head, a.nh), 64 * a.nw, wb * a.nw + extra, st>>>(a);
+  k_attn_dq<BF, DP, SPLIT, LONG><<<(unsigned)item_blocks(a.near, a.per_head, a.nh), 64 * a.nw, wb * a.nw + extra, st>>>(a);
   HGNN_LAUNCH_CHECK("k_attn_dq");
   return HGNN_OK;
 }
 
 template <bool BF, int DP, bool SPLIT>
 int32_t launch_dkv(hipStream_t st, AttnArgs a) {
-  constexpr int WB = FWD_TABLE + dkv_wave_bytes<BF, DP>();
-  const int extra = SPLIT ? join_bytes(DP) : 0;
-  a.nw = SPLIT ? waves_that_fit(WB, extra) : 1;
-  k_attn_dkv<BF, DP, SPLIT><<<(unsigned)(item_blocks(a.near, a.plan.max_tiles, a.nkv) + a.nh), 64 * a.nw, WB * a.nw + extra, st>>>(a);
+  constexpr int WB = TABLE + dkv_wave_bytes<BF, DP>();
+  a.nw = SPLIT ? waves_that_fit(WB, 0) : 1;
+  k_attn_dkv<BF, DP, SPLIT><<<(unsigned)(item_blocks(a.near, a.plan.max_tiles, a.nkv) + a.nh), 64 * a.nw, WB * a.nw, st>>>(a);
   HGNN_LAUNCH_CHECK("k_attn_dkv");
   return HGNN_OK;
 }
@@ -1051,7 +1113,9 @@ int32_t run_width(hipStream_t st, AttnArgs a, bool fwd) {
   a.near = 2.0 * a.N / a.G * a.nkv * a.dh * (BF ? 2 : 4) <= 2e6;
   const bool split = attn_split(a.plan.max_tiles, a.nh, a.G, a.N, 1);
   if (fwd) return split ? launch_fwd<BF, DP, true>(st, a) : launch_fwd<BF, DP, false>(st, a);
-  HGNN_TRY((split ? launch_dq<BF, DP, true>(st, a) : launch_dq<BF, DP, false>(st, a)));
+  if (long_graphs(a.G, a.N)) HGNN_TRY((launch_dq<BF, DP, true, true>(st, a)));
+  else if (split) HGNN_TRY((launch_dq<BF, DP, true, false>(st, a)));
+  else HGNN_TRY((launch_dq<BF, DP, false, false>(st, a)));
   return attn_split(a.plan.max_tiles, a.nkv, a.G, a.N, a.nh / a.nkv) ? launch_dkv<BF, DP, true>(st, a) : launch_dkv<BF, DP, false>(st, a);
 }
 

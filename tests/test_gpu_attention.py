@@ -132,6 +132,21 @@ def test_no_pair_left_out(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,kv,d,nb,rare", [(2, 1, 32, 16, 0.01), (1, 1, 64, 64, 0.02), (2, 2, 8, 2, 0.002), (1, 1, 128, 5, 1.0), (1, 1, 16, 1, 1.0)])
+def test_long_graphs(heads, kv, d, nb, rare, dtype):
+    """Over 1,024 atoms: most tiles have nearly all pairs in the last bucket, some have not (the first rows), some pairs are left out."""
+    P = _problem([1100, 1029], heads, kv, d, nb, dtype, left_out=0.02)
+    rng = np.random.default_rng(nb)
+    where, pitch = ob.pair_layout(P["off"])
+    for k, n in enumerate((1100, 1029)):
+        m = P["pairs"][where[k]:where[k + 1]].reshape(n, pitch[k])
+        common = (rng.random((n, n)) > rare) & (m[:, :n] < nb)
+        common[:40] = False
+        m[:, :n][common] = nb - 1
+    _check(P)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_more_tiles_than_wavefronts(dtype):
     """Many heads: a wavefront takes several tiles, and its sums of the bias gradient run over them."""
     _check(_problem([1 + (5 * i) % 41 for i in range(150)], 64, 16, 8, 9, dtype))
