@@ -141,23 +141,36 @@ __global__ void __launch_bounds__(256) k_norm_fwd(NormArgs a) {
   if (a.saved && lane % LPR == 0) *reinterpret_cast<float4*>(a.saved + row * 4) = make_float4(mu1, r1, mu0, r0);
 }
 
+// Wavefronts per SIMD that the registers of the reverse kernel allow, by the values of a row that a lane holds; as many workgroups
+// per compute unit are launched. (With two for all: 67 us at 40,041 x 256 bf16, and 56 at 7,703 x 866 with one.)
+constexpr int norm_bwd_waves(int values) { return values <= 4 ? 4 : values <= 8 ? 3 : 2; }
+
 template <class T, int LPR, int V, int NC>
-__global__ void __launch_bounds__(256) k_norm_bwd(NormArgs a) {
+__global__ void __launch_bounds__(256, norm_bwd_waves(V * NC)) k_norm_bwd(NormArgs a) {
   constexpr int RPW = 64 / LPR;
+  constexpr bool LP = V * NC > 4;   // the parameters of a lane's columns are kept in LDS, not in registers
   __shared__ float sh[3][NC * LPR * V];
+  __shared__ __align__(16) float sp[LP ? 4 * NC * LPR * V : 1];
   const int lane = threadIdx.x & 63, sub = lane / LPR, wave = threadIdx.x >> 6;
   const int col = (lane % LPR) * V;
   float acc[5][NC][V] = {};
-  float s[NC][V] = {}, w1[NC][V] = {}, c1[NC][V] = {}, w0[NC][V] = {};
+  float own[LP ? 1 : 4][NC][V] = {};
+  if constexpr (LP) {
+    for (int k = 0; k < 4; ++k)
+      for (int j = threadIdx.x; j < a.H; j += 256) sp[k * NC * LPR * V + j] = a.P[k * a.H + j];
+    __syncthreads();
+  } else {
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
-    if (col + c * LPR * V < a.H) {
-      const int o = col + c * LPR * V;
-      load_v<float, V>(a.P + o, s[c]);
-      load_v<float, V>(a.P + a.H + o, w1[c]);
-      load_v<float, V>(a.P + 2 * a.H + o, c1[c]);
-      load_v<float, V>(a.P + 3 * a.H + o, w0[c]);
-    }
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (col + c * LPR * V < a.H) load_v<float, V>(a.P + k * a.H + col + c * LPR * V, own[k][c]);
+  }
+  // parameter k (s, w1, c1, w0) of the lane's column (c, i)
+  auto par = [&](int k, int c, int i) {
+    if constexpr (LP) return sp[k * NC * LPR * V + c * LPR * V + col + i];
+    else return own[k][c][i];
+  };
   const float inv = 1.0f / a.H;
   for (long row = ((long)blockIdx.x * 4 + wave) * RPW + sub; row < a.N; row += (long)gridDim.x * 4 * RPW) {
     const long at = row * a.H + col;
@@ -192,7 +205,7 @@ __global__ void __launch_bounds__(256) k_norm_bwd(NormArgs a) {
         }
       float m = 0.f, mx = 0.f;
       HGNN_EACH(x[c][i] = (x[c][i] - st.z) * st.w; acc[3][c][i] = fmaf(t[c][i], x[c][i], acc[3][c][i]); acc[4][c][i] += t[c][i];
-                t[c][i] *= w0[c][i]; m += t[c][i]; mx = fmaf(t[c][i], x[c][i], mx);)
+                t[c][i] *= par(3, c, i); m += t[c][i]; mx = fmaf(t[c][i], x[c][i], mx);)
       m = a.layer ? row_sum<LPR>(m) * inv : 0.f;
       mx = row_sum<LPR>(mx) * inv;
       HGNN_EACH(g[c][i] += st.w * (t[c][i] - m - x[c][i] * mx);)
@@ -203,10 +216,10 @@ __global__ void __launch_bounds__(256) k_norm_bwd(NormArgs a) {
     if (a.b) {
       float m = 0.f, mx = 0.f, gz = 0.f;
       HGNN_EACH(const float gm = a.gate == HGNN_GATE_CHANNEL ? sigmoid_f(z[c][i]) : ga;
-                const float bh = (b[c][i] - st.x) * st.y, u = fmaf(bh, w1[c][i], c1[c][i]), q = g[c][i] * s[c][i] * gm;
+                const float bh = (b[c][i] - st.x) * st.y, w1 = par(1, c, i), u = fmaf(bh, w1, par(2, c, i)), q = g[c][i] * par(0, c, i) * gm;
                 acc[0][c][i] = fmaf(g[c][i] * gm, u, acc[0][c][i]); acc[1][c][i] = fmaf(q, bh, acc[1][c][i]); acc[2][c][i] += q;
                 z[c][i] = q * u * (1.0f - gm); gz += z[c][i];
-                const float t = q * w1[c][i]; m += t; mx = fmaf(t, bh, mx); g[c][i] = t; b[c][i] = bh;)
+                const float t = q * w1; m += t; mx = fmaf(t, bh, mx); g[c][i] = t; b[c][i] = bh;)
       m = a.layer ? row_sum<LPR>(m) * inv : 0.f;
       mx = row_sum<LPR>(mx) * inv;
       HGNN_EACH(b[c][i] = st.y * (g[c][i] - m - b[c][i] * mx);)
@@ -247,27 +260,40 @@ __global__ void __launch_bounds__(256) k_norm_bwd(NormArgs a) {
   }
 }
 
-// gP[j] = sum over the workgroups' partials, in order within each of 16 runs and then over the runs
+// gP[j] = sum over the workgroups' partials, in order within each of 32 runs and then over the runs
 __global__ void __launch_bounds__(1024) k_norm_reduce(const float* partial, int np, int n, float* gP) {
-  __shared__ float sh[16][64];
-  const int c = threadIdx.x & 63, s = threadIdx.x >> 6, j = blockIdx.x * 64 + c;
-  const int per = (np + 15) / 16, k1 = min(np, (s + 1) * per);
+  __shared__ float sh[32][33];
+  const int c = threadIdx.x & 31, s = threadIdx.x >> 5, j = blockIdx.x * 32 + c;
+  const int per = (np + 31) / 32, k1 = min(np, (s + 1) * per);
   float v = 0.f;
   if (j < n)
-    for (int k = s * per; k < k1; ++k) v += partial[(size_t)k * n + j];
+    for (int k = s * per; k < k1; k += 8) {   // eight loads on their way at a time
+      float t[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) t[u] = k + u < k1 ? partial[(size_t)(k + u) * n + j] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v += t[u];
+    }
   sh[s][c] = v;
   __syncthreads();
   if (s == 0 && j < n) {
-    for (int k = 1; k < 16; ++k) v += sh[k][c];
+    for (int k = 1; k < 32; ++k) v += sh[k][c];
     gP[j] = v;
   }
 }
 
-// workgroups of the reverse pass: two per compute unit hold the chip, fewer where each would have less than one round of rows
+// values of a row that a lane holds, as launch_norm() chooses them
+int norm_values(int H) {
+  if (H % 4 == 0) return H <= 256 ? 4 : H <= 512 ? 8 : 16;
+  if (H % 2 == 0) return H <= 128 ? 2 : H <= 256 ? 4 : H <= 512 ? 8 : 16;
+  return H <= 64 ? 1 : H <= 256 ? 4 : H <= 512 ? 8 : 16;
+}
+
+// workgroups of the reverse pass: as many as run at once, fewer where each would have less than one round of rows
 int norm_bwd_groups(int N, int H) {
   const int rpw = H % 4 == 0 && H <= 64 ? 4 : H % 4 == 0 && H <= 128 ? 2 : 1;
-  const long need = ((long)N + 4 * rpw - 1) / (4 * rpw);
-  return (int)(need < 512 ? need : 512);
+  const long need = ((long)N + 4 * rpw - 1) / (4 * rpw), most = (long)num_cus() * norm_bwd_waves(norm_values(H));
+  return (int)(need < most ? need : most);
 }
 
 // the widest access that every row's start is aligned to, and the lanes and chunks that hold a row
@@ -374,7 +400,7 @@ extern "C" int32_t hgnn_block_norm_bwd(void* stream, int32_t N, int32_t H, int32
     HGNN_LAUNCH_CHECK("k_norm_bwd");
   }
   if (groups != 1) {   // (none: no row, zeros)
-    k_norm_reduce<<<(5 * H + 63) / 64, 1024, 0, st>>>(a.partial, groups, 5 * H, gP);
+    k_norm_reduce<<<(5 * H + 31) / 32, 1024, 0, st>>>(a.partial, groups, 5 * H, gP);
     HGNN_LAUNCH_CHECK("k_norm_reduce");
   }
   return HGNN_OK;
