@@ -5,6 +5,13 @@
 // on how the work is cut: a minimum over values has no ties to break. 12 operations an image and pair, 324 a pair in a
 // periodic graph and 12 otherwise, against one byte written: bound by the vector units. A thread takes four neighbouring pairs
 // of a row (one 4-byte store), a workgroup eight rows, whose positions and images stay in registers and shared memory.
+//
+// In a cell more than twice as high as the last boundary R in every direction, some 35 operations find the one image that can
+// matter: an image vector r* shorter than R has fractional coordinates |f_k| <= |r*| / h_k < 1/2 (h_k: the cell's heights), so rounding
+// the fractional coordinates of any image finds it, and every other image is longer than h_min - R > R. So the pair takes the
+// distance of the rounded image where that is below R, formed as above, and is beyond every boundary where it is not. The margins
+// (1/1000 of R on both sides) are far above the rounding errors for coordinates up to 500 R; a pair with larger ones, or whose
+// rounded image is none of the 27, takes them all. 20,000 atoms: 2.8 ms with 27 images a pair.
 #include "common.h"
 #include "pairs.h"
 #include "prof.h"
@@ -99,16 +106,30 @@ struct BucketArgs {
   uint8_t* pairs;
 };
 
+// number of boundaries that do not exceed d2 (a d2 that is no number: all)
+__device__ __forceinline__ int boundaries_below(const float* edge, int nedge, float d2) {
+  int lo = 0, hi = nedge;
+  while (lo < hi) {
+    const int m = (lo + hi) >> 1;
+    if (d2 < edge[m]) hi = m;
+    else lo = m + 1;
+  }
+  return lo;
+}
+
 // workgroup: 8 rows of a tile; thread: row tid / 32, pairs 4 (tid % 32) .. + 3 of every 128
 __global__ void __launch_bounds__(256) k_pair_buckets(BucketArgs a) {
   __shared__ float4 img[27];
   __shared__ float edge[PAIR_EDGES + 1];
+  __shared__ float inv[9];    // inverse of the cell
+  __shared__ int roomy_s;
   const int tile = blockIdx.x >> 2;
   if (tile >= *a.plan.count) return;
   const PairTile w = a.plan.tile[tile];
   const int g = w.g, lo = w.lo, n = w.n, i0 = w.i0 + (blockIdx.x & 3) * 8;
   if (i0 >= n) return;
   const bool periodic = a.cell && a.pbc && a.pbc[g];
+  const float last2 = a.nedge ? a.edge2[a.nedge - 1] : 0.f, last = sqrtf(last2);
   if (threadIdx.x < 27) {
     float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
     if (periodic) {
@@ -120,6 +141,34 @@ __global__ void __launch_bounds__(256) k_pair_buckets(BucketArgs a) {
     }
     img[threadIdx.x] = t;
   }
+  if (threadIdx.x == 64) {
+    bool roomy = periodic;
+    if (periodic) {
+      const float* c = a.cell + (size_t)g * 9;
+      // columns of the inverse: cross products of the other two rows over the determinant; 1 / their lengths are the heights
+      float x[3][3];
+      for (int k = 0; k < 3; ++k) {
+        const float *u = c + (k + 1) % 3 * 3, *v = c + (k + 2) % 3 * 3;
+        x[k][0] = u[1] * v[2] - u[2] * v[1];
+        x[k][1] = u[2] * v[0] - u[0] * v[2];
+        x[k][2] = u[0] * v[1] - u[1] * v[0];
+      }
+      const float det = (c[0] * x[0][0] + c[1] * x[0][1]) + c[2] * x[0][2];
+      float low = __builtin_inff(), size = 0.f;
+      for (int k = 0; k < 3; ++k) {
+        for (int d = 0; d < 3; ++d) {
+          inv[d * 3 + k] = x[k][d] / det;
+          size = fmaxf(size, fabsf(c[3 * k + d]));
+        }
+        const float height = fabsf(det) / sqrtf((x[k][0] * x[k][0] + x[k][1] * x[k][1]) + x[k][2] * x[k][2]);
+        roomy = roomy && height > 2.01f * last;   // (false for what is no number: a flat cell)
+        low = fminf(low, height);
+      }
+      // (in a cell much longer than high the fractional coordinates lose their accuracy)
+      roomy = roomy && size < 100.f * low && size < 500.f * last;
+    }
+    roomy_s = roomy;
+  }
   for (int e = threadIdx.x; e < a.nedge; e += 256) edge[e] = a.edge2[e];
   __syncthreads();
   const int i = i0 + (threadIdx.x >> 5);
@@ -128,34 +177,58 @@ __global__ void __launch_bounds__(256) k_pair_buckets(BucketArgs a) {
   const float px = p[0], py = p[1], pz = p[2];
   const int64_t pitch = pair_pitch(n);
   uint8_t* row = a.pairs + w.off + i * pitch;
-  const int first = periodic ? 0 : 13, last = periodic ? 26 : 13;
-  for (int j = (threadIdx.x & 31) * 4; j < pitch; j += 128) {
-    float q[4][3], best[4];
+  const bool roomy = roomy_s;
+  const int first = periodic ? 0 : 13, past = periodic ? 27 : 14;
+  float v[9], c[9];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int jj = j + k < n ? j + k : n - 1;
-      const float* s = a.pos + ((size_t)lo + jj) * 3;
-      q[k][0] = s[0]; q[k][1] = s[1]; q[k][2] = s[2];
-      best[k] = __builtin_inff();
-    }
-    for (int m = first; m <= last; ++m) {
-      const float4 t = img[m];
+  for (int k = 0; k < 9; ++k) v[k] = inv[k];
+  if (roomy) {
+#pragma unroll
+    for (int k = 0; k < 9; ++k) c[k] = a.cell[(size_t)g * 9 + k];
+  }
+  const float far2 = last2 * 1.002f, most = 500.f * last;
+  const bool small = fmaxf(fmaxf(fabsf(px), fabsf(py)), fabsf(pz)) < most;
+  for (int j = (threadIdx.x & 31) * 4; j < pitch; j += 128) {
+    float q[4][3];
+    if (j + 4 <= n) {
+      __builtin_memcpy(q, a.pos + ((size_t)lo + j) * 3, 48);
+    } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float x = px - (q[k][0] + t.x), y = py - (q[k][1] + t.y), z = pz - (q[k][2] + t.z);
-        best[k] = fminf(best[k], (x * x + y * y) + z * z);
+        const float* s = a.pos + ((size_t)lo + (j + k < n ? j + k : n - 1)) * 3;
+        q[k][0] = s[0]; q[k][1] = s[1]; q[k][2] = s[2];
       }
     }
     unsigned out = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      int lo_e = 0, hi_e = a.nedge;   // boundaries below lo_e are <= best, boundaries from hi_e on are above it
-      while (lo_e < hi_e) {
-        const int m = (lo_e + hi_e) >> 1;
-        if (best[k] < edge[m]) hi_e = m;
-        else lo_e = m + 1;
+      int m0 = first, m1 = past;   // images to look at
+      if (roomy) {
+        const float x = px - q[k][0], y = py - q[k][1], z = pz - q[k][2];
+        float s[3];
+#pragma unroll
+        for (int d = 0; d < 3; ++d) s[d] = rintf(__builtin_fmaf(x, v[d], __builtin_fmaf(y, v[3 + d], z * v[6 + d])));
+        const float rx = __builtin_fmaf(-s[0], c[0], __builtin_fmaf(-s[1], c[3], __builtin_fmaf(-s[2], c[6], x)));
+        const float ry = __builtin_fmaf(-s[0], c[1], __builtin_fmaf(-s[1], c[4], __builtin_fmaf(-s[2], c[7], y)));
+        const float rz = __builtin_fmaf(-s[0], c[2], __builtin_fmaf(-s[1], c[5], __builtin_fmaf(-s[2], c[8], z)));
+        const float r2 = __builtin_fmaf(rx, rx, __builtin_fmaf(ry, ry, rz * rz));
+        const float shift = fmaxf(fmaxf(fabsf(s[0]), fabsf(s[1])), fabsf(s[2])), size = fmaxf(fmaxf(fabsf(q[k][0]), fabsf(q[k][1])), fabsf(q[k][2]));
+        if (small && size < most && shift <= 1.f) {
+          m0 = 13 + (int)s[0] * 9 + (int)s[1] * 3 + (int)s[2];
+          m1 = r2 < far2 ? m0 + 1 : m0;
+        }
       }
-      const unsigned b = j + k >= n || (a.drop_far && lo_e == a.nedge) ? (unsigned)HGNN_PAIR_NONE : (unsigned)lo_e;
+      unsigned b = a.nedge;
+      if (m0 < m1) {
+        float best = __builtin_inff();
+        for (int m = m0; m < m1; ++m) {
+          const float4 t = img[m];
+          const float x = px - (q[k][0] + t.x), y = py - (q[k][1] + t.y), z = pz - (q[k][2] + t.z);
+          best = fminf(best, (x * x + y * y) + z * z);
+        }
+        b = boundaries_below(edge, a.nedge, best);
+      }
+      if (j + k >= n || (a.drop_far && b == (unsigned)a.nedge)) b = HGNN_PAIR_NONE;
       out |= b << (8 * k);
     }
     *reinterpret_cast<unsigned*>(row + j) = out;

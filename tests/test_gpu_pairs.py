@@ -42,6 +42,41 @@ def test_buckets(kind, nedge, drop):
         assert np.array_equal(got.cpu().numpy(), ob.pair_buckets(pos, off, c, p, edge2, drop)) and untouched(guard)
 
 
+@pytest.mark.parametrize("drop", [False, True])
+@pytest.mark.parametrize("tall", [12.03, 12.1, 30.0])
+def test_cells_more_than_twice_as_high_as_the_last_boundary(tall, drop):
+    """Where one image per pair is looked at: heights just above (and below) twice the last boundary, ties between images, atoms on the
+    faces, outside the cell and far away, pairs at a boundary's very distance."""
+    import torch
+    from paper_2506_21788_amd import binding as B
+    rng = np.random.default_rng(int(tall * 10))
+    edge = np.array([1.0, 2.5, 4.0, 6.0], np.float32)
+    cells = np.stack([np.diag([tall, tall, tall]), np.diag([tall, 40.0, 17.0]), tall * np.eye(3) + np.tril(rng.random((3, 3)) * 4, -1),
+                      np.diag([11.9, 30.0, 30.0]), tall * np.eye(3)[[1, 2, 0]]]).astype(np.float32)
+    n = np.array([150, 97, 200, 64, 33])
+    off = np.concatenate([[0], np.cumsum(n)]).astype(np.int32)
+    N, G = int(off[-1]), len(n)
+    frac = rng.random((N, 3))
+    frac[::4] = np.round(frac[::4] * 4) / 4
+    frac[5] += 1.0                                   # outside the cell by one, by three, and far away
+    frac[6] -= 3.0
+    pos = np.einsum("na,nab->nb", frac, cells[np.repeat(np.arange(G), n)].astype(np.float64)).astype(np.float32)
+    pos[7] += 2.0e4
+    pos[10] = pos[9] + np.array([6.0, 0, 0], np.float32)
+    pos[12] = pos[11] + np.array([0, 5.9999995, 0], np.float32)
+    pos[14] = np.nan
+    plan = torch.empty(B.pair_plan_workspace_bytes(N, G), dtype=torch.uint8, device="cuda")
+    got, guard = room(B.pair_plan(N, G, dev(off, "i32"), plan))
+    B.pair_buckets(N, G, plan, dev(pos), dev(cells), dev(np.ones(G), "u8"), 4, dev(edge ** 2), drop, got)
+    want = ob.pair_buckets(np.where(np.isnan(pos), np.float32(1e18), pos), off, cells, np.ones(G), edge ** 2, drop)
+    assert untouched(guard)
+    where, pitch = ob.pair_layout(off)
+    m = want[:where[1]].reshape(150, pitch[0])
+    beyond = 255 if drop else 4
+    m[14, :150] = m[:, 14] = beyond                  # (also to itself)
+    assert np.array_equal(got.cpu().numpy(), want)
+
+
 def test_distance_that_is_no_number_is_beyond_every_boundary():
     import torch
     from paper_2506_21788_amd import binding as B
