@@ -854,25 +854,26 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : BF &
   }
 }
 
-// g_bias of head h: the workgroups' partials in order, a run per group of threads, then the runs
+// g_bias of head h: the workgroups' partials in order, a run per group of threads (8 to 64, as many as there are buckets), then the runs
 __device__ __forceinline__ void bias_reduce(const AttnArgs& a, int h, float* sh) {
-  const int b = threadIdx.x & 63, run = threadIdx.x >> 6, runs = blockDim.x >> 6;
+  const int w = a.nb <= 8 ? 8 : a.nb <= 16 ? 16 : a.nb <= 32 ? 32 : 64;
+  const int b = threadIdx.x & (w - 1), run = threadIdx.x / w, runs = blockDim.x / w;
   const int per = (a.per_head + runs - 1) / runs, k1 = min(a.per_head, (run + 1) * per);
   float s = 0.f;
   if (b < a.nb) {
     const float* p = a.partial + (size_t)h * a.per_head * a.nb + b;
-    for (int k = run * per; k < k1; k += 16) {   // sixteen loads on their way at a time
-      float v[16];
+    for (int k = run * per; k < k1; k += 32) {   // 32 loads on their way at a time: the chain of their waits is the kernel's on small batches
+      float v[32];
 #pragma unroll
-      for (int u = 0; u < 16; ++u) v[u] = k + u < k1 ? p[(size_t)(k + u) * a.nb] : 0.f;
+      for (int u = 0; u < 32; ++u) v[u] = p[(size_t)min(k + u, k1 - 1) * a.nb];
 #pragma unroll
-      for (int u = 0; u < 16; ++u) s += v[u];
+      for (int u = 0; u < 32; ++u) s += k + u < k1 ? v[u] : 0.f;
     }
   }
   sh[threadIdx.x] = s;
   __syncthreads();
   if (run == 0 && b < a.nb) {
-    for (int k = 1; k < runs; ++k) s += sh[k * 64 + b];
+    for (int k = 1; k < runs; ++k) s += sh[k * w + b];
     if (a.bias[(size_t)h * a.nb + b] == -__builtin_inff()) s = 0.f;   // its pairs are left out
     a.g_bias[(size_t)h * a.nb + b] = s;
   }

@@ -631,9 +631,9 @@ __global__ void __launch_bounds__(256) k_dense_reduce(const float* partial, cons
   for (int k = 0; k < nsplit; k += 8) {
     float v[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) v[u] = k + u < nsplit ? p[(k + u) * stride] : 0.f;
+    for (int u = 0; u < 8; ++u) v[u] = p[min(k + u, nsplit - 1) * stride];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) s += v[u];
+    for (int u = 0; u < 8; ++u) s += k + u < nsplit ? v[u] : 0.f;
   }
   *out = s;
 }

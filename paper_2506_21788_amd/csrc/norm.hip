@@ -270,9 +270,9 @@ __global__ void __launch_bounds__(1024) k_norm_reduce(const float* partial, int 
     for (int k = s * per; k < k1; k += 8) {   // eight loads on their way at a time
       float t[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) t[u] = k + u < k1 ? partial[(size_t)(k + u) * n + j] : 0.f;
+      for (int u = 0; u < 8; ++u) t[u] = partial[(size_t)min(k + u, k1 - 1) * n + j];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) v += t[u];
+      for (int u = 0; u < 8; ++u) v += k + u < k1 ? t[u] : 0.f;
     }
   sh[s][c] = v;
   __syncthreads();

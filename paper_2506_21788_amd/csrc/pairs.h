@@ -20,9 +20,7 @@ struct alignas(32) PairTile {
 
 struct PairPlan {
   int32_t* count;         // [1] tiles in all; 0 if the offsets were refused
-  int64_t* pair_off;      // [G] first byte of every graph's matrix
-  int32_t* tile_off;      // [G+1] tiles of PAIR_T atoms before every graph
-  PairTile* tile;         // [max_tiles]
+  PairTile* tile;         // [max_tiles] graph after graph
   int64_t max_tiles;      // what N atoms in G graphs can at most make
   size_t bytes;
 };
@@ -32,8 +30,6 @@ inline PairPlan pair_plan_view(const void* plan, int32_t N, int32_t G) {
   PairPlan v;
   v.max_tiles = (int64_t)N / PAIR_T + (G < N ? G : N);
   v.count = c.take<int32_t>(1);
-  v.pair_off = c.take<int64_t>((size_t)G);
-  v.tile_off = c.take<int32_t>((size_t)G + 1);
   v.tile = c.take<PairTile>((size_t)v.max_tiles);
   v.bytes = c.used();
   return v;

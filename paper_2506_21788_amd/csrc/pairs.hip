@@ -21,8 +21,10 @@ namespace {
 
 constexpr int PAIR_EDGES = 254;   // most boundaries: buckets 0..254, byte 255 is HGNN_PAIR_NONE
 
-// one workgroup: running sums over the graphs, the check of the offsets, the total for the host
+// One workgroup: running sums over the graphs, the check of the offsets, every tile's record, the total for the host. A thread writes the
+// records of its graph's first tiles, a wavefront those of its long graphs.
 __global__ void __launch_bounds__(1024) k_pair_plan(int N, int G, const int32_t* graph_off, PairPlan v, HostMail* mail) {
+  constexpr int OWN = 8;
   __shared__ long long wb[16];
   __shared__ int wt[16], bad_s;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -36,13 +38,16 @@ __global__ void __launch_bounds__(1024) k_pair_plan(int N, int G, const int32_t*
     const int g = g0 + tid;
     long long bytes = 0;
     int tiles = 0;
+    PairTile r{};
     if (g < G) {
       const int lo = graph_off[g], hi = graph_off[g + 1];
       if (lo < 0 || hi < lo || hi > N) bad = 1;
       else {
-        const long long n = hi - lo;
-        bytes = n * pair_pitch(n);
-        tiles = (int)((n + PAIR_T - 1) / PAIR_T);
+        r.lo = lo;
+        r.n = hi - lo;
+        r.g = g;
+        bytes = r.n * pair_pitch(r.n);
+        tiles = (r.n + PAIR_T - 1) / PAIR_T;
       }
     }
     long long ib = bytes;
@@ -62,9 +67,24 @@ __global__ void __launch_bounds__(1024) k_pair_plan(int N, int G, const int32_t*
       tb += wb[w];
       tt += wt[w];
     }
-    if (g < G) {
-      v.pair_off[g] = pb + ib - bytes;
-      v.tile_off[g] = pt + it - tiles;
+    r.off = pb + ib - bytes;
+    const int t0 = pt + it - tiles;
+    // (offsets that are refused below may name more tiles than there is room for)
+    for (int k = 0; k < OWN && k < tiles; ++k) {
+      r.i0 = k * PAIR_T;
+      if ((unsigned)(t0 + k) < (unsigned)v.max_tiles) v.tile[t0 + k] = r;
+    }
+    for (unsigned long long m = __ballot(tiles > OWN); m; m &= m - 1) {
+      const int l = __ffsll(m) - 1, s0 = __shfl(t0, l), ns = __shfl(tiles, l);
+      PairTile q{};
+      q.off = __shfl(r.off, l);
+      q.lo = __shfl(r.lo, l);
+      q.n = __shfl(r.n, l);
+      q.g = __shfl(r.g, l);
+      for (int k = OWN + lane; k < ns; k += 64) {
+        q.i0 = k * PAIR_T;
+        if ((unsigned)(s0 + k) < (unsigned)v.max_tiles) v.tile[s0 + k] = q;
+      }
     }
     base_b += tb;
     base_t += tt;
@@ -73,29 +93,9 @@ __global__ void __launch_bounds__(1024) k_pair_plan(int N, int G, const int32_t*
   if (bad) atomicOr(&bad_s, 1);
   __syncthreads();
   if (tid == 0) {
-    v.tile_off[G] = base_t;
     *v.count = bad_s ? 0 : base_t;
     post_mail(mail, base_b, bad_s);
   }
-}
-
-// every tile's record: a binary search for its graph
-__global__ void __launch_bounds__(256) k_pair_tiles(int G, const int32_t* graph_off, PairPlan v) {
-  const int t = blockIdx.x * 256 + threadIdx.x;
-  if (t >= *v.count) return;
-  int lo = 0, hi = G;   // tile_off[lo] <= t < tile_off[hi]
-  while (hi - lo > 1) {
-    const int m = (lo + hi) >> 1;
-    if (v.tile_off[m] <= t) lo = m;
-    else hi = m;
-  }
-  PairTile r{};
-  r.off = v.pair_off[lo];
-  r.lo = graph_off[lo];
-  r.n = graph_off[lo + 1] - r.lo;
-  r.i0 = (t - v.tile_off[lo]) * PAIR_T;
-  r.g = lo;
-  v.tile[t] = r;
 }
 
 struct BucketArgs {
@@ -266,10 +266,6 @@ extern "C" int32_t hgnn_pair_plan(void* stream, int32_t N, int32_t G, const int3
     ProfScope ps(PT_MISC, st);
     k_pair_plan<<<1, 1024, 0, st>>>(N, G, graph_off, v, mail.dev());
     HGNN_LAUNCH_CHECK("k_pair_plan");
-    if (v.max_tiles > 0) {
-      k_pair_tiles<<<(unsigned)((v.max_tiles + 255) / 256), 256, 0, st>>>(G, graph_off, v);
-      HGNN_LAUNCH_CHECK("k_pair_tiles");
-    }
   }
   HGNN_HIP(mail.wait());
   HGNN_REQUIRE(mail.status() == 0, HGNN_ERR_BAD_OFFSETS, "graph_off must start at 0, not decrease and end at N");
