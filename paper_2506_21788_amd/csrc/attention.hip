@@ -166,13 +166,13 @@ struct Tile {
   using T = typename Row<BF, DP>::T;
   static constexpr int EP = 16 / sizeof(T), NP = DP / EP;   // elements of a piece, pieces of a row
   u32x4_t f[NP / 2];
-  // p: the tile's first row (uniform); rows: how many exist (the last one stands for those behind it)
+  // p: the tile's first row (uniform); rows: how many exist (the last one stands for those behind it, and a row's last piece for
+  // those behind that: the operand that meets it in a product has zeros there, and result columns past dh are not stored)
   __device__ __forceinline__ void load(const T* p, unsigned ld, int rows, int dh, int lane) {
 #pragma unroll
     for (int u = 0; u < NP / 2; ++u) {
-      const int row = (u * 64 + lane) / NP, d = (u * 64 + lane) % NP * EP;
-      f[u] = u32x4_t{0, 0, 0, 0};
-      if (d < dh) f[u] = *reinterpret_cast<const u32x4_t*>(p + (unsigned)(min(row, rows - 1) * ld + d));
+      const int row = (u * 64 + lane) / NP, d = min((u * 64 + lane) % NP * EP, dh - EP);
+      f[u] = *reinterpret_cast<const u32x4_t*>(p + (unsigned)(min(row, rows - 1) * ld + d));
     }
   }
   __device__ __forceinline__ void to_lds(T* tile, int lane) const {
@@ -342,17 +342,15 @@ __device__ __forceinline__ u32x4_t load_buckets(const uint8_t* at, int j0, int n
   return w;
 }
 
-// a bias in units of the product, -inf for what is no bucket. A finite one stays finite: a row of the lowest values is still a
-// softmax over its pairs.
-__device__ __forceinline__ float table_value(const float* bias, int nb, int b, float inv) {
-  if (b >= nb) return -__builtin_inff();
-  const float x = bias[b], v = x * inv;
-  return fabsf(x) < __builtin_inff() ? fminf(fmaxf(v, -3.4028235e38f), 3.4028235e38f) : v;
-}
-// 256 of them, by one wavefront
-__device__ __forceinline__ void fill_table(float* table, const float* bias, int nb, float inv, int lane) {
+// The table of one head's biases in units of the product: 256 entries, -inf for what is no bucket (a wavefront fills its own, or the
+// same as the others). A finite bias stays finite: a row of the lowest values is still a softmax over its pairs. In two
+// steps, so that the wait for the biases does not hold up the loads behind it.
+__device__ __forceinline__ float read_bias(const float* bias, int nb, int lane) { return bias[min(lane, nb - 1)]; }   // (nb <= 64)
+__device__ __forceinline__ void fill_table(float* table, float x, int nb, float inv, int lane) {
+  const float v = fabsf(x) < __builtin_inff() ? fminf(fmaxf(x * inv, -3.4028235e38f), 3.4028235e38f) : x;
+  table[lane] = lane < nb ? v : -__builtin_inff();
 #pragma unroll
-  for (int k = 0; k < 4; ++k) table[k * 64 + lane] = table_value(bias, nb, k * 64 + lane, inv);
+  for (int k = 1; k < 4; ++k) table[k * 64 + lane] = -__builtin_inff();
 }
 __device__ __forceinline__ f32x16_t biases(unsigned table, const u32x4_t& w) {
   f32x16_t t;
@@ -498,8 +496,7 @@ __global__ void __launch_bounds__(256, DP == 128 ? 1 : 2) k_attn_fwd(AttnArgs a)
   float* table = reinterpret_cast<float*>(smem);
   T* tk = reinterpret_cast<T*>(smem + TABLE + wave * fwd_wave_bytes<BF, DP>());
   T* tv = tk + 32 * Row<BF, DP>::PITCH;
-  fill_table(table, a.bias + (size_t)h * a.nb, a.nb, a.inv, lane);   // (SPLIT: the same values by every wavefront)
-  lds_order();
+  const float my_bias = read_bias(a.bias + (size_t)h * a.nb, a.nb, lane);
 
   const int hk = h / (a.nh / a.nkv);
   const unsigned ld = (unsigned)(a.nh + 2 * a.nkv) * a.dh;   // elements of an atom's q, k, v
@@ -525,6 +522,7 @@ __global__ void __launch_bounds__(256, DP == 128 ? 1 : 2) k_attn_fwd(AttnArgs a)
   const float slack = 8.f / a.c;
   int j0 = wave * PAIR_T;
   if (j0 < w.n) fetch(j0);
+  fill_table(table, my_bias, a.nb, a.inv, lane);   // (SPLIT: the same values by every wavefront)
   for (; j0 < w.n; j0 += step) {
     lds_order();
     kt.to_lds(tk, lane);
@@ -693,9 +691,8 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : BF &
   T* tv = tk + 32 * Row<BF, DP>::PITCH;
   const unsigned hist0 = TABLE + wave * wave_bytes + 2 * tile_bytes<BF, DP>();
   float* hist = reinterpret_cast<float*>(smem + hist0);
-  fill_table(table, a.bias + (size_t)h * a.nb, a.nb, a.inv, lane);
+  const float my_bias = read_bias(a.bias + (size_t)h * a.nb, a.nb, lane);
   for (int b = lane; b < (a.nb + 1) * COLS; b += 64) hist[b] = 0.f;
-  lds_order();
   const unsigned col = hist0 + (lane & (COLS - 1)) * 4;
   float far_sum = 0.f;
   const int hk = h / (a.nh / a.nkv);
@@ -711,10 +708,7 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : BF &
     q.load(base + (size_t)w.i0 * ld + (size_t)h * a.dh + ql * ld, a.dh, g);
     const size_t orow = ((size_t)w.lo + w.i0) * lo_ + (size_t)h * a.dh;
     go.load(static_cast<const T*>(a.g_out) + orow + ql * lo_, a.dh, g);
-    float D = go.dot32((BF ? a.o32 : static_cast<const float*>(a.out)) + orow + ql * lo_, a.dh, g);
-    D += other_half(D);
-    const float2 st = real ? a.stat[(size_t)h * a.N + w.lo + qi] : make_float2(0.f, __builtin_inff());
-    if (real && g == 0 && wave == 0) a.delta[(size_t)h * a.N + w.lo + qi] = D;
+    float2 st = a.stat[(size_t)h * a.N + w.lo + w.i0 + ql];
     const T* kbase = base + (size_t)(a.nh + hk) * a.dh;
     const uint8_t* prow = w.pairs + w.i0 * w.pitch;
     const T* vbase = kbase + (size_t)a.nkv * a.dh;
@@ -733,6 +727,11 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : BF &
     const int step = SPLIT ? a.nw * PAIR_T : PAIR_T;
     int j0 = wave * PAIR_T;
     if (j0 < w.n) fetch(j0);
+    float D = go.dot32((BF ? a.o32 : static_cast<const float*>(a.out)) + orow + ql * lo_, a.dh, g);
+    D += other_half(D);
+    if (!real) st = make_float2(0.f, __builtin_inff());
+    if (real && g == 0 && wave == 0) a.delta[(size_t)h * a.N + w.lo + qi] = D;
+    if (t == me) fill_table(table, my_bias, a.nb, a.inv, lane);
     for (; j0 < w.n; j0 += step) {
       lds_order();
       kt.to_lds(tk, lane);
@@ -921,9 +920,7 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k
   for (int r = 0; r < rep; ++r, i0 -= span) {
     if (i0 >= span) continue;
     const int h = hk * rep + r;
-    lds_order();
-    fill_table(table, a.bias + (size_t)h * a.nb, a.nb, a.inv, lane);
-    lds_order();
+    const float my_bias = read_bias(a.bias + (size_t)h * a.nb, a.nb, lane);
     Tile<BF, DP> qt, gt;
     u32x4_t bk;
     float2 st;
@@ -940,6 +937,8 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k
       if (part && (lane & 31) > (int)il) st = make_float2(0.f, __builtin_inff());   // a row past the last atom: weight 0
     };
     fetch(i0);
+    lds_order();
+    fill_table(table, my_bias, a.nb, a.inv, lane);
     for (; i0 < w.n; i0 += step) {
       lds_order();
       qt.to_lds(tq, lane);
@@ -996,7 +995,7 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k
     for (int u = 0; u < rep; ++u) {
       const int h = hk * rep + u;
       lds_order();
-      fill_table(table, a.bias + (size_t)h * a.nb, a.nb, a.inv, lane);
+      fill_table(table, read_bias(a.bias + (size_t)h * a.nb, a.nb, lane), a.nb, a.inv, lane);
       lds_order();
       for (int i = 0; i < w.n; ++i) {
         const float b = table[w.pairs[i * w.pitch + w.i0 + r]];
