@@ -360,7 +360,7 @@ int32_t hgnn_multihead_deep_bwd(void* stream, int32_t N, int32_t G, int32_t H, i
  * `saved` (size from the query; NULL: no reverse pass follows) is written by _fwd and read by _bwd.
  * _bwd takes x_out (x where b was NULL), g_x_out = dL/dx' past this seam's y (NULL = 0) and g_y (NULL where y was) and writes
  * g_x, g_b, g_z and gP (zeros for what does not take part). x_out may alias x, g_x may alias g_x_out; no other aliasing.
- * 1 <= H <= 1024. Errors: BAD_SHAPE for any other H, an unknown norm, gate or dtype, eps < 0, a gate without b.
+ * 1 <= H <= 1024, N below 2^26 (else OVERFLOW). Errors: BAD_SHAPE for any other H, an unknown norm, gate or dtype, eps < 0, a gate without b.
  * WORKSPACE_TOO_SMALL if ws or saved is smaller than the query says. Only enqueues work.
  * ------------------------------------------------------------------------------------------- */
 int32_t hgnn_block_norm_workspace_bytes(int32_t N, int32_t H, size_t* ws_bytes_host, size_t* saved_bytes_host);
@@ -411,7 +411,7 @@ int32_t hgnn_pair_buckets(void* stream, int32_t N, int32_t G, const void* plan, 
  * `saved` (NULL: no reverse pass follows) is written by _fwd and read by _bwd with the same out. plan: hgnn_pair_plan of this
  * batch; pairs: a pair matrix of it (its padding is not looked at).
  * 1 <= nh <= 64, nkv divides nh, dh a multiple of 8 in 8..128, 1 <= nb <= 64, 1e-6 <= scale <= 1e6 (else BAD_SHAPE). N and G below 2^28, and
- * (N / 32 + min(N, G) + 64) nh below 2^31 (else OVERFLOW). Only enqueue work.
+ * (N / 32 + min(N, G) + 64) nh below 2^26 (else OVERFLOW). Only enqueue work.
  * dtype HGNN_BF16 rounds p and ds to bfloat16 where they enter the products of g_q, g_k and g_v; out, g_bias and all softmax
  * statistics are formed without such a rounding.
  * ------------------------------------------------------------------------------------------- */

@@ -1058,6 +1058,8 @@ AttnSaved carve_attn_saved(void* p, int N, int nh, int dh, bool bf16) {
   return s;
 }
 
+constexpr int64_t MOST_THREADS = (int64_t)1 << 32;   // of a launch: it has to have fewer
+
 int32_t check_attn(int32_t N, int32_t G, int32_t nh, int32_t nkv, int32_t dh, int32_t nb, int32_t dtype) {
   HGNN_REQUIRE(N >= 0 && G >= 0, HGNN_ERR_BAD_SHAPE, "negative N or G");
   HGNN_REQUIRE(nh >= 1 && nh <= 64 && nkv >= 1 && nh % nkv == 0, HGNN_ERR_BAD_SHAPE,
@@ -1066,7 +1068,7 @@ int32_t check_attn(int32_t N, int32_t G, int32_t nh, int32_t nkv, int32_t dh, in
   HGNN_REQUIRE(nb >= 1 && nb <= ATTN_BUCKETS, HGNN_ERR_BAD_SHAPE, "graph_attention: 1..%d buckets (got %d)", ATTN_BUCKETS, nb);
   HGNN_REQUIRE(dtype == HGNN_F32 || dtype == HGNN_BF16, HGNN_ERR_BAD_SHAPE, "unknown dtype %d", dtype);
   HGNN_REQUIRE(N < (1 << 28) && G < (1 << 28), HGNN_ERR_OVERFLOW, "graph_attention: N and G must be below 2^28");
-  HGNN_REQUIRE((pair_plan_view(nullptr, N, G).max_tiles + 64) * nh < INT_MAX, HGNN_ERR_OVERFLOW, "graph_attention: too many tiles for one launch");
+  HGNN_REQUIRE((pair_plan_view(nullptr, N, G).max_tiles + 64) * nh < MOST_THREADS / 64, HGNN_ERR_OVERFLOW, "graph_attention: too many tiles for one launch");
   return HGNN_OK;
 }
 
@@ -1074,9 +1076,11 @@ int32_t check_attn(int32_t N, int32_t G, int32_t nh, int32_t nkv, int32_t dh, in
 // wavefront per SIMD this shortens the chain of tiles without taking a compute unit from anybody. Long graphs: 2,500
 // wavefronts of 625 tiles each leave a fifth of the SIMDs idle at the end; four times as many of a quarter the length do not, and
 // the join is small against their chains.
-// Where keys are shared by query heads, k_attn_dkv has few and long chains as well.
+// Where keys are shared by query heads, k_attn_dkv has few and long chains as well. (Never where a launch could not hold four
+// wavefronts a tile.)
 bool long_graphs(int64_t G, int64_t N) { return N >= 1024 * G; }
 bool attn_split(int64_t max_tiles, int heads, int64_t G, int64_t N, int rep) {
+  if ((max_tiles + 64) * (heads * rep) >= MOST_THREADS / 256) return false;
   return (max_tiles * heads <= 4 * num_cus() && N * rep > 2 * PAIR_T * G) || long_graphs(G, N) || rep > 1;
 }
 

@@ -328,6 +328,7 @@ void launch_norm(hipStream_t st, const NormArgs& a, int groups) {
 
 int32_t check_norm(int32_t N, int32_t H, int32_t norm, int32_t gate, int32_t dtype) {
   HGNN_REQUIRE(N >= 0, HGNN_ERR_BAD_SHAPE, "negative N");
+  HGNN_REQUIRE(N < (1 << 26), HGNN_ERR_OVERFLOW, "block_norm: N must be below 2^26 (a launch has fewer than 2^32 threads)");
   HGNN_REQUIRE(H >= 1 && H <= 1024, HGNN_ERR_BAD_SHAPE, "block_norm: H must be in 1..1024 (got %d)", H);
   HGNN_REQUIRE(norm == HGNN_NORM_RMS || norm == HGNN_NORM_LAYER, HGNN_ERR_BAD_SHAPE, "unknown norm %d", norm);
   HGNN_REQUIRE(gate == HGNN_GATE_NONE || gate == HGNN_GATE_ATOM || gate == HGNN_GATE_CHANNEL, HGNN_ERR_BAD_SHAPE, "unknown gate %d", gate);

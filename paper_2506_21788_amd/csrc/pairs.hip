@@ -99,7 +99,8 @@ __global__ void __launch_bounds__(1024) k_pair_plan(int N, int G, const int32_t*
 }
 
 struct BucketArgs {
-  int G, nedge, drop_far;
+  int nedge, drop_far;
+  int64_t first;          // first tile of this launch
   const float *pos, *cell, *edge2;
   const uint8_t* pbc;
   PairPlan plan;
@@ -123,7 +124,7 @@ __global__ void __launch_bounds__(256) k_pair_buckets(BucketArgs a) {
   __shared__ float edge[PAIR_EDGES + 1];
   __shared__ float inv[9];    // inverse of the cell
   __shared__ int roomy_s;
-  const int tile = blockIdx.x >> 2;
+  const int64_t tile = a.first + (blockIdx.x >> 2);
   if (tile >= *a.plan.count) return;
   const PairTile w = a.plan.tile[tile];
   const int g = w.g, lo = w.lo, n = w.n, i0 = w.i0 + (blockIdx.x & 3) * 8;
@@ -283,10 +284,14 @@ extern "C" int32_t hgnn_pair_buckets(void* stream, int32_t N, int32_t G, const v
   BucketArgs a{};
   a.plan = pair_plan_view(plan, N, G);
   HGNN_REQUIRE(plan_bytes >= a.plan.bytes, HGNN_ERR_WORKSPACE_TOO_SMALL, "pair plan: need %zu bytes, got %zu", a.plan.bytes, plan_bytes);
-  a.G = G; a.nedge = nedge; a.drop_far = drop_far; a.pos = pos; a.cell = cell; a.edge2 = edge2; a.pbc = pbc; a.pairs = pairs;
+  a.nedge = nedge; a.drop_far = drop_far; a.pos = pos; a.cell = cell; a.edge2 = edge2; a.pbc = pbc; a.pairs = pairs;
   hipStream_t st = static_cast<hipStream_t>(stream);
   ProfScope ps(PT_MISC, st);
-  k_pair_buckets<<<(unsigned)(a.plan.max_tiles * 4), 256, 0, st>>>(a);
-  HGNN_LAUNCH_CHECK("k_pair_buckets");
+  constexpr int64_t MOST = (1 << 22) - 1;   // tiles of a launch, which has to have fewer than 2^32 threads
+  for (a.first = 0; a.first < a.plan.max_tiles; a.first += MOST) {
+    const int64_t left = a.plan.max_tiles - a.first;
+    k_pair_buckets<<<(unsigned)((left < MOST ? left : MOST) * 4), 256, 0, st>>>(a);
+    HGNN_LAUNCH_CHECK("k_pair_buckets");
+  }
   return HGNN_OK;
 }

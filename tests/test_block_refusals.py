@@ -106,3 +106,15 @@ def test_dense():
         assert bwd(**kw) == code, kw
     assert lib.hgnn_round_bf16(None, i64(-1), P, P) == SHAPE and lib.hgnn_round_bf16(None, i64(4), None, P) == NULL
     assert lib.hgnn_round_bf16(None, i64(1 << 42), P, P) == OVERFLOW and lib.hgnn_round_bf16(None, i64(0), None, None) == 0
+
+
+def test_more_rows_and_tiles_than_a_launch_can_hold():
+    lib = _lib()
+    a, b = sz(0), sz(0)
+    norm = lambda N: lib.hgnn_block_norm_workspace_bytes(i32(N), i32(8), ctypes.byref(a), ctypes.byref(b))  # noqa: E731
+    assert norm((1 << 26) - 1) == 0 and norm(1 << 26) == OVERFLOW
+    assert lib.hgnn_block_norm_fwd(None, i32(1 << 26), i32(8), i32(0), i32(0), i32(0), f32(1e-5), P, P, None, P, P, P, None, sz(0)) == OVERFLOW
+    # 2^22 graphs of one atom: 2^22 + 2^17 tiles, 2^32 threads and more with 16 heads and a wavefront each
+    att = lambda nh: lib.hgnn_graph_attention_workspace_bytes(i32(1 << 22), i32(1 << 22), i32(nh), i32(1), i32(8), i32(1), i32(0), ctypes.byref(a),  # noqa: E731
+                                                              ctypes.byref(b))
+    assert att(15) == 0 and att(16) == OVERFLOW

@@ -293,3 +293,34 @@ def test_offsets_past_32_bits():
     want = ob.graph_attention(sub["qkv"], bias.double().cpu().numpy(), m, sub["off"], 1, 1, 0.35, sub["g"])
     for a, w in zip((out[n - 50:], g_qkv[n - 50:], g_bias), want):
         assert np.allclose(a.double().cpu().numpy(), w, rtol=1e-4, atol=1e-5)
+
+
+def test_more_tiles_than_one_launch_of_four_wavefronts_holds():
+    """Graphs of one atom: an atom attends to itself alone, so the output is its value, D = g . v, and q and k have no gradient."""
+    import torch
+    from paper_2506_21788_amd import binding as B
+    N, nh, nkv, d = 4_300_000, 8, 4, 8          # 4.4 million tiles; times 4 key heads and 256 threads: more than 2^32
+    off = torch.arange(N + 1, dtype=torch.int32, device="cuda")
+    plan = torch.empty(B.pair_plan_workspace_bytes(N, N), dtype=torch.uint8, device="cuda")
+    size = B.pair_plan(N, N, off, plan)
+    assert size == 32 * N
+    pairs = torch.full((size,), 7, dtype=torch.uint8, device="cuda")
+    pos = torch.zeros((N, 3), device="cuda")
+    edge2 = torch.tensor([1.0], device="cuda")
+    B.pair_buckets(N, N, plan, pos, None, None, 1, edge2, False, pairs)
+    p = pairs.view(N, 32)
+    assert not p[:, 0].any() and (p[:, 1:] == B.PAIR_NONE).all()
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    qkv, g = torch.randn((N, nh + 2 * nkv, d), device="cuda", generator=gen), torch.randn((N, nh, d), device="cuda", generator=gen)
+    bias = torch.zeros((nh, 2), device="cuda")
+    ws_b, saved_b = B.graph_attention_workspace_bytes(N, N, nh, nkv, d, 2, B.F32)
+    ws, saved = (torch.empty(k, dtype=torch.uint8, device="cuda") for k in (ws_b, saved_b))
+    out, g_qkv, g_bias = torch.full_like(g, 9.0), torch.full_like(qkv, 9.0), torch.empty_like(bias)
+    B.graph_attention_fwd(N, N, nh, nkv, d, 2, B.F32, 0.35, plan, pairs, qkv, bias, out, saved)
+    B.graph_attention_bwd(N, N, nh, nkv, d, 2, B.F32, 0.35, plan, pairs, qkv, bias, out, saved, g, g_qkv, g_bias, ws)
+    torch.cuda.synchronize()
+    # the exponent c (s - m) of the only pair is formed as c s - c m, a few steps of 2^-24 of |c m| <= 64 from 0, and divides out of
+    # the output again; the reverse weight 2^(c s - c m - log2 l) keeps such an error
+    assert torch.allclose(out, qkv[:, nh + nkv:].repeat_interleave(2, 1), rtol=8 * 2.0 ** -24, atol=0)
+    assert torch.allclose(g_qkv[:, nh + nkv:], g.view(N, nkv, 2, d).sum(2), rtol=1e-5, atol=2e-5)
+    assert g_qkv[:, :nh + nkv].abs().max() < 1e-3
