@@ -6,12 +6,14 @@
 // periodic graph and 12 otherwise, against one byte written: bound by the vector units. A thread takes four neighbouring pairs
 // of a row (one 4-byte store), a workgroup eight rows, whose positions and images stay in registers and shared memory.
 //
-// In a cell more than twice as high as the last boundary R in every direction, some 35 operations find the one image that can
-// matter: an image vector r* shorter than R has fractional coordinates |f_k| <= |r*| / h_k < 1/2 (h_k: the cell's heights), so rounding
-// the fractional coordinates of any image finds it, and every other image is longer than h_min - R > R. So the pair takes the
-// distance of the rounded image where that is below R, formed as above, and is beyond every boundary where it is not. The margins
-// (1/1000 of R on both sides) are far above the rounding errors for coordinates up to 500 R; a pair with larger ones, or whose
-// rounded image is none of the 27, takes them all. 20,000 atoms: 2.8 ms with 27 images a pair.
+// In a cell more than twice as high as the last boundary R in every direction some 14 operations rule out most pairs: an image vector
+// r* shorter than R has fractional coordinates |f_k| <= |r*| / h_k < 1/2 (h_k: the cell's heights), so rounding the difference of the
+// atoms' fractional coordinates to whole numbers s finds that image, and the rest |d_k| <= R / h_k in every direction. A pair
+// that fails this is beyond every boundary. The others are few (all pairs of 20,000 atoms at 75 R^3 an atom: 4 %), so a wavefront lists
+// them and forms their distances afterwards with full lanes: that of the image s where that is one of the 27 (every other image is
+// longer than h_min - R > R), of all of them where it is not. The margins (1/1000 of R and of the cell) cover the rounding of the
+// fractional coordinates, of which cells up to 16 times as long as high and coordinates up to 100 R are good to 5e-4; a pair with larger
+// coordinates takes all images. A thread has the fractional coordinates of four atoms for eight rows.
 #include "common.h"
 #include "pairs.h"
 #include "prof.h"
@@ -118,16 +120,133 @@ __device__ __forceinline__ int boundaries_below(const float* edge, int nedge, fl
   return lo;
 }
 
-// workgroup: 8 rows of a tile; thread: row tid / 32, pairs 4 (tid % 32) .. + 3 of every 128
+// squared distance over the images m0 .. m1 - 1
+__device__ __forceinline__ float nearest(const float4* img, int m0, int m1, float px, float py, float pz, float qx, float qy, float qz) {
+  float best = __builtin_inff();
+  for (int m = m0; m < m1; ++m) {
+    const float4 t = img[m];
+    const float x = px - (qx + t.x), y = py - (qy + t.y), z = pz - (qz + t.z);
+    best = fminf(best, (x * x + y * y) + z * z);
+  }
+  return best;
+}
+
+constexpr int ROWS = 8, COLS = 256;   // of a workgroup; of a wavefront at a time
+
+// what a roomy cell gives: columns of the inverse, the most that a rest may be in each direction
+struct Roomy {
+  float inv[9], rest[3];
+  int yes;
+};
+__device__ __forceinline__ void fractional(const Roomy& c, const float (&p)[3], float (&f)[3]) {
+#pragma unroll
+  for (int d = 0; d < 3; ++d) f[d] = __builtin_fmaf(p[0], c.inv[d], __builtin_fmaf(p[1], c.inv[3 + d], p[2] * c.inv[6 + d]));
+}
+__device__ __forceinline__ bool moderate(const float (&p)[3], float most) {   // (false for what is no number)
+  return fabsf(p[0]) < most && fabsf(p[1]) < most && fabsf(p[2]) < most;
+}
+
+struct Rows {
+  float4 f[ROWS];   // fractional coordinates; w: 1 where they are not to be used
+  float4 p[ROWS];
+};
+
+// Pairs of ROWS rows of a roomy cell. A wavefront's items: COLS columns of all rows, or of some where there are few columns.
+__device__ __forceinline__ void roomy_rows(const BucketArgs& a, const PairTile& w, int i0, const Roomy& cell, float last, const float4* img, const float* edge,
+                                           Rows& rows, unsigned short* list, unsigned* out) {
+  const int n = w.n, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nrows = min(ROWS, n - i0);
+  const int64_t pitch = pair_pitch(n);
+  const float most = 100.f * last;
+  uint8_t* base = a.pairs + w.off + i0 * pitch;
+  const float* pos = a.pos + (size_t)w.lo * 3;
+  const unsigned far = a.drop_far ? (unsigned)HGNN_PAIR_NONE : (unsigned)a.nedge;
+  const Roomy c = cell;
+  if (lane < ROWS) {   // (the same by every wavefront)
+    const float* s = pos + (size_t)min(i0 + lane, n - 1) * 3;
+    const float p[3] = {s[0], s[1], s[2]};
+    float f[3];
+    fractional(c, p, f);
+    rows.f[lane] = make_float4(f[0], f[1], f[2], moderate(p, most) ? 0.f : 1.f);
+    rows.p[lane] = make_float4(p[0], p[1], p[2], 0.f);
+  }
+  auto order = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local"); __builtin_amdgcn_wave_barrier(); };
+  const int chunks = (int)((pitch + COLS - 1) / COLS), parts = chunks >= 4 ? 1 : 4, per = ROWS / parts;
+  for (int item = wave; item < chunks * parts; item += 4) {
+    const int j0 = item / parts * COLS, r0 = item % parts * per, r1 = min(nrows, r0 + per), j = j0 + lane * 4;
+    float f[4][3];
+    bool wild[4];
+    unsigned word = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float* s = pos + (size_t)min(j + k, n - 1) * 3;
+      const float q[3] = {s[0], s[1], s[2]};
+      fractional(c, q, f[k]);
+      wild[k] = !moderate(q, most);
+      if (j + k >= n) {   // padding: no number is near
+        f[k][0] = __builtin_nanf("");
+        wild[k] = false;
+      }
+      word |= (j + k < n ? far : (unsigned)HGNN_PAIR_NONE) << (8 * k);
+    }
+    int count = 0;
+    order();
+    for (int r = r0; r < r1; ++r) {
+      const float4 i = rows.f[r];
+      const bool all = i.w != 0.f;
+      out[r * 64 + lane] = word;
+      bool near[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float x = i.x - f[k][0], y = i.y - f[k][1], z = i.z - f[k][2];
+        const int close = (int)(fabsf(x - rintf(x)) <= c.rest[0]) & (int)(fabsf(y - rintf(y)) <= c.rest[1]) & (int)(fabsf(z - rintf(z)) <= c.rest[2]);
+        near[k] = (close | (int)wild[k] | ((int)all & (int)(j + k < n))) != 0;
+      }
+      if (__ballot(near[0] | near[1] | near[2] | near[3])) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const unsigned long long m = __ballot(near[k]);
+          if (near[k]) list[count + __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0))] = (unsigned short)(r * COLS + lane * 4 + k);
+          count += __popcll(m);
+        }
+      }
+    }
+    order();
+    for (int e = lane; e < count; e += 64) {
+      const int at = list[e];
+      const float4 i = rows.f[at / COLS], p = rows.p[at / COLS];
+      const float* s = pos + (size_t)(j0 + at % COLS) * 3;
+      const float q[3] = {s[0], s[1], s[2]};
+      float g[3];
+      fractional(c, q, g);
+      const float s0 = rintf(i.x - g[0]), s1 = rintf(i.y - g[1]), s2 = rintf(i.z - g[2]);
+      int m0 = 0, m1 = 27;
+      if (i.w == 0.f && moderate(q, most) && fmaxf(fmaxf(fabsf(s0), fabsf(s1)), fabsf(s2)) <= 1.f) {
+        m0 = 13 + (int)s0 * 9 + (int)s1 * 3 + (int)s2;
+        m1 = m0 + 1;
+      }
+      const unsigned b = boundaries_below(edge, a.nedge, nearest(img, m0, m1, p.x, p.y, p.z, q[0], q[1], q[2]));
+      reinterpret_cast<uint8_t*>(out)[at] = (uint8_t)(b == (unsigned)a.nedge ? far : b);
+    }
+    order();
+    for (int e = lane; e < (r1 - r0) * (COLS / 16); e += 64) {
+      const int r = r0 + e / (COLS / 16), piece = e % (COLS / 16);
+      if (j0 + piece * 16 < pitch) *reinterpret_cast<uint4*>(base + r * pitch + j0 + piece * 16) = *reinterpret_cast<const uint4*>(out + r * 64 + piece * 4);
+    }
+  }
+}
+
+// workgroup: 8 rows of a tile. Cells that are not roomy: thread: row tid / 32, pairs 4 (tid % 32) .. + 3 of every 128
 __global__ void __launch_bounds__(256) k_pair_buckets(BucketArgs a) {
   __shared__ float4 img[27];
   __shared__ float edge[PAIR_EDGES + 1];
-  __shared__ float inv[9];    // inverse of the cell
-  __shared__ int roomy_s;
+  __shared__ Roomy cell;
+  __shared__ Rows rows;
+  __shared__ unsigned short list[4][ROWS * COLS];
+  __shared__ __align__(16) unsigned words[4][ROWS * COLS / 4];
   const int64_t tile = a.first + (blockIdx.x >> 2);
   if (tile >= *a.plan.count) return;
   const PairTile w = a.plan.tile[tile];
-  const int g = w.g, lo = w.lo, n = w.n, i0 = w.i0 + (blockIdx.x & 3) * 8;
+  const int g = w.g, lo = w.lo, n = w.n, i0 = w.i0 + (blockIdx.x & 3) * ROWS;
   if (i0 >= n) return;
   const bool periodic = a.cell && a.pbc && a.pbc[g];
   const float last2 = a.nedge ? a.edge2[a.nedge - 1] : 0.f, last = sqrtf(last2);
@@ -158,37 +277,33 @@ __global__ void __launch_bounds__(256) k_pair_buckets(BucketArgs a) {
       float low = __builtin_inff(), size = 0.f;
       for (int k = 0; k < 3; ++k) {
         for (int d = 0; d < 3; ++d) {
-          inv[d * 3 + k] = x[k][d] / det;
+          cell.inv[d * 3 + k] = x[k][d] / det;
           size = fmaxf(size, fabsf(c[3 * k + d]));
         }
         const float height = fabsf(det) / sqrtf((x[k][0] * x[k][0] + x[k][1] * x[k][1]) + x[k][2] * x[k][2]);
         roomy = roomy && height > 2.01f * last;   // (false for what is no number: a flat cell)
+        cell.rest[k] = 1.001f * last / height + 0.001f;
         low = fminf(low, height);
       }
       // (in a cell much longer than high the fractional coordinates lose their accuracy)
-      roomy = roomy && size < 100.f * low && size < 500.f * last;
+      roomy = roomy && size < 16.f * low && size < 100.f * last;
     }
-    roomy_s = roomy;
+    cell.yes = roomy;
   }
   for (int e = threadIdx.x; e < a.nedge; e += 256) edge[e] = a.edge2[e];
   __syncthreads();
+  if (cell.yes) {   // uniform over the workgroup
+    const int wave = threadIdx.x >> 6;
+    roomy_rows(a, w, i0, cell, last, img, edge, rows, list[wave], words[wave]);
+    return;
+  }
   const int i = i0 + (threadIdx.x >> 5);
   if (i >= n) return;
   const float* p = a.pos + ((size_t)lo + i) * 3;
   const float px = p[0], py = p[1], pz = p[2];
   const int64_t pitch = pair_pitch(n);
   uint8_t* row = a.pairs + w.off + i * pitch;
-  const bool roomy = roomy_s;
   const int first = periodic ? 0 : 13, past = periodic ? 27 : 14;
-  float v[9], c[9];
-#pragma unroll
-  for (int k = 0; k < 9; ++k) v[k] = inv[k];
-  if (roomy) {
-#pragma unroll
-    for (int k = 0; k < 9; ++k) c[k] = a.cell[(size_t)g * 9 + k];
-  }
-  const float far2 = last2 * 1.002f, most = 500.f * last;
-  const bool small = fmaxf(fmaxf(fabsf(px), fabsf(py)), fabsf(pz)) < most;
   for (int j = (threadIdx.x & 31) * 4; j < pitch; j += 128) {
     float q[4][3];
     if (j + 4 <= n) {
@@ -203,32 +318,7 @@ __global__ void __launch_bounds__(256) k_pair_buckets(BucketArgs a) {
     unsigned out = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      int m0 = first, m1 = past;   // images to look at
-      if (roomy) {
-        const float x = px - q[k][0], y = py - q[k][1], z = pz - q[k][2];
-        float s[3];
-#pragma unroll
-        for (int d = 0; d < 3; ++d) s[d] = rintf(__builtin_fmaf(x, v[d], __builtin_fmaf(y, v[3 + d], z * v[6 + d])));
-        const float rx = __builtin_fmaf(-s[0], c[0], __builtin_fmaf(-s[1], c[3], __builtin_fmaf(-s[2], c[6], x)));
-        const float ry = __builtin_fmaf(-s[0], c[1], __builtin_fmaf(-s[1], c[4], __builtin_fmaf(-s[2], c[7], y)));
-        const float rz = __builtin_fmaf(-s[0], c[2], __builtin_fmaf(-s[1], c[5], __builtin_fmaf(-s[2], c[8], z)));
-        const float r2 = __builtin_fmaf(rx, rx, __builtin_fmaf(ry, ry, rz * rz));
-        const float shift = fmaxf(fmaxf(fabsf(s[0]), fabsf(s[1])), fabsf(s[2])), size = fmaxf(fmaxf(fabsf(q[k][0]), fabsf(q[k][1])), fabsf(q[k][2]));
-        if (small && size < most && shift <= 1.f) {
-          m0 = 13 + (int)s[0] * 9 + (int)s[1] * 3 + (int)s[2];
-          m1 = r2 < far2 ? m0 + 1 : m0;
-        }
-      }
-      unsigned b = a.nedge;
-      if (m0 < m1) {
-        float best = __builtin_inff();
-        for (int m = m0; m < m1; ++m) {
-          const float4 t = img[m];
-          const float x = px - (q[k][0] + t.x), y = py - (q[k][1] + t.y), z = pz - (q[k][2] + t.z);
-          best = fminf(best, (x * x + y * y) + z * z);
-        }
-        b = boundaries_below(edge, a.nedge, best);
-      }
+      unsigned b = boundaries_below(edge, a.nedge, nearest(img, first, past, px, py, pz, q[k][0], q[k][1], q[k][2]));
       if (j + k >= n || (a.drop_far && b == (unsigned)a.nedge)) b = HGNN_PAIR_NONE;
       out |= b << (8 * k);
     }

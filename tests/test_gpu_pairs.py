@@ -77,6 +77,35 @@ def test_cells_more_than_twice_as_high_as_the_last_boundary(tall, drop):
     assert np.array_equal(got.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("n", [200, 257, 1031, 1300])
+@pytest.mark.parametrize("shape", ["cube", "oblique", "long"])
+def test_roomy_cells_of_many_columns(shape, n):
+    """Several runs of 256 columns of a roomy cell, the last one cut; oblique cells and ones 15 times as long as high; pairs on the
+    boundary between two images; atoms whose fractional coordinates are not to be trusted among the others."""
+    import torch
+    from paper_2506_21788_amd import binding as B
+    rng = np.random.default_rng(n + len(shape))
+    edge = np.array([0.5, 1.0, 1.7, 2.0], np.float32)
+    cell = {"cube": 9.0 * np.eye(3), "oblique": np.array([[9.0, 0, 0], [7.0, 6, 0], [-5, 4, 6]]), "long": np.array([[60.0, 0, 0], [11, 4.6, 0], [-20, 1.5, 4.7]])}[shape]
+    frac = rng.random((n, 3))
+    frac[::3] = np.round(frac[::3] * 2) / 2
+    frac[1::7] += rng.integers(-1, 2, (len(frac[1::7]), 3))
+    pos = (frac @ cell).astype(np.float32)
+    pos[n // 2] += 250.0                               # more than 100 boundaries away
+    pos[n - 1] -= 1.0e6
+    pos[3] = pos[5]
+    off = np.array([0, n], np.int32)
+    plan = torch.empty(B.pair_plan_workspace_bytes(n, 1), dtype=torch.uint8, device="cuda")
+    size = B.pair_plan(n, 1, dev(off, "i32"), plan)
+    cell = cell.astype(np.float32)[None]
+    for drop in (False, True):
+        got, guard = room(size)
+        B.pair_buckets(n, 1, plan, dev(pos), dev(cell), dev(np.ones(1), "u8"), 4, dev(edge ** 2), drop, got)
+        want = ob.pair_buckets(pos, off, cell, np.ones(1), edge ** 2, drop)
+        assert np.array_equal(got.cpu().numpy(), want) and untouched(guard)
+        assert (want < (4 if not drop else 255)).sum() > 2 * n     # (there is something to find)
+
+
 def test_distance_that_is_no_number_is_beyond_every_boundary():
     import torch
     from paper_2506_21788_amd import binding as B
