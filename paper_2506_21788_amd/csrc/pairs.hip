@@ -6,7 +6,7 @@
 // periodic graph and 12 otherwise, against one byte written: bound by the vector units. A thread takes four neighbouring pairs
 // of a row (one 4-byte store), a workgroup eight rows, whose positions and images stay in registers and shared memory.
 //
-// In a cell more than twice as high as the last boundary R in every direction some 14 operations rule out most pairs: an image vector
+// In a cell more than twice as high as the last boundary R in every direction some ten operations rule out most pairs: an image vector
 // r* shorter than R has fractional coordinates |f_k| <= |r*| / h_k < 1/2 (h_k: the cell's heights), so rounding the difference of the
 // atoms' fractional coordinates to whole numbers s finds that image, and the rest |d_k| <= R / h_k in every direction. A pair
 // that fails this is beyond every boundary. The others are few (all pairs of 20,000 atoms at 75 R^3 an atom: 4 %), so a wavefront lists
@@ -133,9 +133,10 @@ __device__ __forceinline__ float nearest(const float4* img, int m0, int m1, floa
 
 constexpr int ROWS = 8, COLS = 256;   // of a workgroup; of a wavefront at a time
 
-// what a roomy cell gives: columns of the inverse, the most that a rest may be in each direction
+// what a roomy cell gives: columns of the inverse, the most that a rest may be in each direction (in 2^-32)
 struct Roomy {
-  float inv[9], rest[3];
+  float inv[9];
+  unsigned rest[3];
   int yes;
 };
 __device__ __forceinline__ void fractional(const Roomy& c, const float (&p)[3], float (&f)[3]) {
@@ -146,9 +147,13 @@ __device__ __forceinline__ bool moderate(const float (&p)[3], float most) {   //
   return fabsf(p[0]) < most && fabsf(p[1]) < most && fabsf(p[2]) < most;
 }
 
+// fractional part in 2^-32: differences of two wrap around as the rounding to the next whole number asks
+__device__ __forceinline__ unsigned turns(float f) { return (unsigned)fminf((f - floorf(f)) * 4294967296.0f, 4294967040.0f); }
+
 struct Rows {
   float4 f[ROWS];   // fractional coordinates; w: 1 where they are not to be used
   float4 p[ROWS];
+  uint4 t[ROWS];    // f in turns, plus the most that a rest may be
 };
 
 // Pairs of ROWS rows of a roomy cell. A wavefront's items: COLS columns of all rows, or of some where there are few columns.
@@ -168,47 +173,60 @@ __device__ __forceinline__ void roomy_rows(const BucketArgs& a, const PairTile& 
     fractional(c, p, f);
     rows.f[lane] = make_float4(f[0], f[1], f[2], moderate(p, most) ? 0.f : 1.f);
     rows.p[lane] = make_float4(p[0], p[1], p[2], 0.f);
+    rows.t[lane] = make_uint4(turns(f[0]) + c.rest[0], turns(f[1]) + c.rest[1], turns(f[2]) + c.rest[2], 0);
   }
   auto order = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local"); __builtin_amdgcn_wave_barrier(); };
+  order();
+  const bool wild_rows = __any(lane < ROWS && rows.f[lane & (ROWS - 1)].w != 0.f);
   const int chunks = (int)((pitch + COLS - 1) / COLS), parts = chunks >= 4 ? 1 : 4, per = ROWS / parts;
   for (int item = wave; item < chunks * parts; item += 4) {
     const int j0 = item / parts * COLS, r0 = item % parts * per, r1 = min(nrows, r0 + per), j = j0 + lane * 4;
-    float f[4][3];
-    bool wild[4];
-    unsigned word = 0;
+    if (r0 >= r1) continue;
+    unsigned u[4][3], word = 0;
+    // a bit per pair, row after row from the highest of `bits` down; columns that exist; pairs to take whatever their coordinates
+    const int bits = (r1 - r0) * 4;
+    unsigned near = 0, exist = 0, wild = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const float* s = pos + (size_t)min(j + k, n - 1) * 3;
       const float q[3] = {s[0], s[1], s[2]};
-      fractional(c, q, f[k]);
-      wild[k] = !moderate(q, most);
-      if (j + k >= n) {   // padding: no number is near
-        f[k][0] = __builtin_nanf("");
-        wild[k] = false;
-      }
+      float f[3];
+      fractional(c, q, f);
+#pragma unroll
+      for (int d = 0; d < 3; ++d) u[k][d] = turns(f[d]);
+      const unsigned column = 0x88888888u >> k;
+      exist |= j + k < n ? column : 0u;
+      wild |= moderate(q, most) ? 0u : column;
       word |= (j + k < n ? far : (unsigned)HGNN_PAIR_NONE) << (8 * k);
     }
-    int count = 0;
     order();
     for (int r = r0; r < r1; ++r) {
-      const float4 i = rows.f[r];
-      const bool all = i.w != 0.f;
+      const uint4 i = rows.t[r];
       out[r * 64 + lane] = word;
-      bool near[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float x = i.x - f[k][0], y = i.y - f[k][1], z = i.z - f[k][2];
-        const int close = (int)(fabsf(x - rintf(x)) <= c.rest[0]) & (int)(fabsf(y - rintf(y)) <= c.rest[1]) & (int)(fabsf(z - rintf(z)) <= c.rest[2]);
-        near[k] = (close | (int)wild[k] | ((int)all & (int)(j + k < n))) != 0;
+        const int close = (int)(i.x - u[k][0] <= 2 * c.rest[0]) & (int)(i.y - u[k][1] <= 2 * c.rest[1]) & (int)(i.z - u[k][2] <= 2 * c.rest[2]);
+        near = near + near + close;
       }
-      if (__ballot(near[0] | near[1] | near[2] | near[3])) {
+    }
+    if (wild_rows) {
+      for (int r = r0; r < r1; ++r)
+        if (rows.f[r].w != 0.f) wild |= 0xfu << (bits - 4 - (r - r0) * 4);
+    }
+    near = (near | wild) & exist & (0xffffffffu >> (32 - bits));
+    int before = __popc(near);   // entries of the lanes up to this one, then of those before it
+    const int mine = before;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const unsigned long long m = __ballot(near[k]);
-          if (near[k]) list[count + __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0))] = (unsigned short)(r * COLS + lane * 4 + k);
-          count += __popcll(m);
-        }
-      }
+    for (int d = 1; d < 64; d <<= 1) {
+      const int t = __shfl_up(before, d);
+      if (lane >= d) before += t;
+    }
+    const int count = __shfl(before, 63);
+    before -= mine;
+    while (near) {
+      const int at = bits - 1 - (31 - __clz(near));
+      list[before++] = (unsigned short)((r0 + at / 4) * COLS + lane * 4 + at % 4);
+      near &= ~(0x80000000u >> __clz(near));
     }
     order();
     for (int e = lane; e < count; e += 64) {
@@ -282,7 +300,7 @@ __global__ void __launch_bounds__(256) k_pair_buckets(BucketArgs a) {
         }
         const float height = fabsf(det) / sqrtf((x[k][0] * x[k][0] + x[k][1] * x[k][1]) + x[k][2] * x[k][2]);
         roomy = roomy && height > 2.01f * last;   // (false for what is no number: a flat cell)
-        cell.rest[k] = 1.001f * last / height + 0.001f;
+        cell.rest[k] = (unsigned)(fminf(1.001f * last / height + 0.001f, 0.4999f) * 4294967296.0f);   // (below 1/2 in a roomy cell)
         low = fminf(low, height);
       }
       // (in a cell much longer than high the fractional coordinates lose their accuracy)
