@@ -672,12 +672,15 @@ __device__ __forceinline__ int bytes_unlike(unsigned w, unsigned v) {
   return __popc((((t & 0x7f7f7f7fu) + 0x7f7f7f7fu) | t) & 0x80808080u);
 }
 
+// wavefronts that a SIMD's registers hold of the reverse kernel over queries
+constexpr int dq_waves(bool bf16, int dp) { return dp == 128 || (!bf16 && dp == 64) ? 1 : bf16 && dp == 32 ? 3 : 2; }
+
 // -------------------------------------------------------------------------------------------------------------------------
 // g_q of 32 queries, D of theirs, and g_bias. A workgroup of head h takes tiles me, me + per_head, ...
 // LONG (graphs of 1,024 atoms and more, SPLIT): nearly all pairs of most tiles are in the last bucket. Those are added up in a register,
 // the few others one by one in LDS, where an addition takes some three cycles a lane that takes part.
 template <bool BF, int DP, bool SPLIT, bool LONG>
-__global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : BF && DP == 32 ? 3 : 2) k_attn_dq(AttnArgs a) {
+__global__ void __launch_bounds__(256, dq_waves(BF, DP)) k_attn_dq(AttnArgs a) {
   using T = typename Row<BF, DP>::T;
   constexpr int COLS = LONG ? 32 : 64;
   extern __shared__ __align__(16) char smem[];
@@ -1025,10 +1028,22 @@ int waves_that_fit(int wave_bytes, int extra) {
   return nw >= 4 ? 4 : nw >= 2 ? 2 : 1;
 }
 
-// workgroups per head of the reverse kernel over queries: every tile its own while they are few, then as many as keep the chip
-// busy (each leaves one partial of g_bias)
-int64_t dq_per_head(int64_t max_tiles, int nh) {
-  const int64_t most = (4096 + nh - 1) / nh;
+// Long graphs: see attn_split.
+bool long_graphs(int64_t G, int64_t N) { return N >= 1024 * G; }
+
+// Workgroups per head of that kernel (each leaves one partial of g_bias): every tile its own while they are few, then as many as run
+// at once, which registers and LDS (160 KB, given out in pieces of 1,280 bytes) decide. (40,041 atoms in 390 graphs, 8 heads, bf16: 62 us; 72 with a tenth more, 67 with half as
+// many more, 72 with a workgroup per tile.) In long graphs, where a tile is a long chain, 4,096 and more are dealt out best.
+int64_t dq_per_head(int64_t max_tiles, int32_t N, int32_t G, int nh, int dh, int nb, bool bf16) {
+  int64_t at_once = 4096;
+  if (!long_graphs(G, N)) {
+    const int dp = dh <= 32 ? 32 : dh <= 64 ? 64 : 128;
+    const int lds = TABLE + (bf16 ? dp == 32 ? dq_wave_bytes<true, 32, 64>(nb) : dp == 64 ? dq_wave_bytes<true, 64, 64>(nb) : dq_wave_bytes<true, 128, 64>(nb)
+                                  : dp == 32 ? dq_wave_bytes<false, 32, 64>(nb) : dp == 64 ? dq_wave_bytes<false, 64, 64>(nb) : dq_wave_bytes<false, 128, 64>(nb));
+    const int by_lds = 128 / ((lds + 1279) / 1280), by_registers = 4 * dq_waves(bf16, dp);
+    at_once = (int64_t)num_cus() * (by_lds < by_registers ? by_lds : by_registers);
+  }
+  const int64_t most = at_once / nh;
   return max_tiles < most ? max_tiles : most;
 }
 
@@ -1036,11 +1051,11 @@ struct AttnWs {
   float *delta, *partial;
   size_t bytes;
 };
-AttnWs carve_attn_ws(void* p, int N, int G, int nh, int nb) {
+AttnWs carve_attn_ws(void* p, int N, int G, int nh, int dh, int nb, bool bf16) {
   Carver c(p);
   AttnWs w;
   w.delta = c.take<float>((size_t)nh * N);
-  w.partial = c.take<float>((size_t)nh * dq_per_head(pair_plan_view(nullptr, N, G).max_tiles, nh) * nb);
+  w.partial = c.take<float>((size_t)nh * dq_per_head(pair_plan_view(nullptr, N, G).max_tiles, N, G, nh, dh, nb, bf16) * nb);
   w.bytes = c.used();
   return w;
 }
@@ -1078,7 +1093,6 @@ int32_t check_attn(int32_t N, int32_t G, int32_t nh, int32_t nkv, int32_t dh, in
 // the join is small against their chains.
 // Where keys are shared by query heads, k_attn_dkv has few and long chains as well. (Never where a launch could not hold four
 // wavefronts a tile.)
-bool long_graphs(int64_t G, int64_t N) { return N >= 1024 * G; }
 bool attn_split(int64_t max_tiles, int heads, int64_t G, int64_t N, int rep) {
   if ((max_tiles + 64) * (heads * rep) >= MOST_THREADS / 256) return false;
   return (max_tiles * heads <= 4 * num_cus() && N * rep > 2 * PAIR_T * G) || long_graphs(G, N) || rep > 1;
@@ -1150,7 +1164,7 @@ extern "C" int32_t hgnn_graph_attention_workspace_bytes(int32_t N, int32_t G, in
                                                         int32_t dtype, size_t* ws_bytes_host, size_t* saved_bytes_host) {
   HGNN_TRY(check_attn(N, G, nh, nkv, dh, nb, dtype));
   HGNN_REQUIRE(ws_bytes_host && saved_bytes_host, HGNN_ERR_NULLPTR, "null size pointer");
-  *ws_bytes_host = carve_attn_ws(nullptr, N, G, nh, nb).bytes;
+  *ws_bytes_host = carve_attn_ws(nullptr, N, G, nh, dh, nb, dtype == HGNN_BF16).bytes;
   *saved_bytes_host = carve_attn_saved(nullptr, N, nh, dh, dtype == HGNN_BF16).bytes;
   return HGNN_OK;
 }
@@ -1197,10 +1211,10 @@ extern "C" int32_t hgnn_graph_attention_bwd(void* stream, int32_t N, int32_t G, 
   HGNN_REQUIRE(plan_bytes >= a.plan.bytes, HGNN_ERR_WORKSPACE_TOO_SMALL, "pair plan: need %zu bytes, got %zu", a.plan.bytes, plan_bytes);
   const AttnSaved s = carve_attn_saved(const_cast<void*>(saved), N, nh, dh, dtype == HGNN_BF16);
   HGNN_REQUIRE(saved_bytes >= s.bytes, HGNN_ERR_WORKSPACE_TOO_SMALL, "graph_attention saved buffer: need %zu bytes, got %zu", s.bytes, saved_bytes);
-  const AttnWs w = carve_attn_ws(ws, N, G, nh, nb);
+  const AttnWs w = carve_attn_ws(ws, N, G, nh, dh, nb, dtype == HGNN_BF16);
   HGNN_REQUIRE(ws_bytes >= w.bytes, HGNN_ERR_WORKSPACE_TOO_SMALL, "graph_attention workspace: need %zu bytes, got %zu", w.bytes, ws_bytes);
   a.N = N; a.G = G; a.nh = nh; a.nkv = nkv; a.dh = dh; a.nb = nb;
-  a.per_head = (int)dq_per_head(a.plan.max_tiles, nh);
+  a.per_head = (int)dq_per_head(a.plan.max_tiles, N, G, nh, dh, nb, dtype == HGNN_BF16);
   a.scale = scale; a.c = scale * LOG2E; a.inv = 1.0f / scale;
   a.pairs = pairs; a.qkv = qkv; a.bias = bias; a.out = const_cast<void*>(out); a.stat = s.stat; a.o32 = s.o32;
   a.g_out = g_out; a.g_qkv = g_qkv; a.delta = w.delta; a.partial = w.partial; a.g_bias = g_bias;
