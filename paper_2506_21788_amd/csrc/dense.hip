@@ -16,6 +16,10 @@
 // workgroup, half of the LDS traffic and of the splitting was W's, and the LDS was what bound the kernel (128 x 128 x 64:
 // 768 cycles of LDS against 512 of the matrix cores). The forward pass lays out W^T for the reverse pass as well, in `saved`.
 //
+// Bound by memory in bf16 (40,041 x 256 -> 512 with silu: 42 us forward, 40 and 36 in reverse, each moving 143 MB: 3.4 to 4.0 TB/s) and
+// by the matrix cores in float32 (7,703 x 866 -> 889 with gelu: 114, 104 and 97 us, six products of 11.9 GFLOP each:
+// 0.63 to 0.74 PFLOP/s, with the splitting on the vector units beside them).
+//
 // Small calls (few tiles) take k_dense_small: 32 x 32 results, the contraction dealt to the four wavefronts of a workgroup, operands
 // straight from memory: nothing is staged, the chain is one load, some products and a join.
 #include <climits>

@@ -10,7 +10,7 @@ namespace hgnn {
 constexpr int PAIR_T = 32;   // atoms of a tile: the edge of a matrix-core tile
 
 // What a kernel has to know of a tile, in one load: with the graph's number alone its place took two more, each waiting for the one
-// before (attention over 390 structures, 13,000 wavefronts of a few tiles each: see k_attn_fwd)
+// before, in each of the 13,000 wavefronts of attention over 390 graphs
 struct alignas(32) PairTile {
   int64_t off;        // first byte of the graph's matrix
   int32_t lo, n;      // the graph's first atom, its atoms
