@@ -1024,18 +1024,35 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k
 }
 
 // -------------------------------------------------------------------------------------------------------------------------
-constexpr int LDS_MOST = 64 * 1024;   // of a workgroup, so that two fit a compute unit and no attribute has to be set
-
-int waves_that_fit(int wave_bytes, int extra) {
-  const int nw = (LDS_MOST - extra) / wave_bytes;
-  return nw >= 4 ? 4 : nw >= 2 ? 2 : 1;
+// Wavefronts of a workgroup that share a tile, of `items` workgroups: one to four, whichever takes the least time by this count: a
+// workgroup's time is its share of a tile, and a compute unit takes `fit` of them at a time, with half a turn idle at the end where
+// there is more than one. simd: wavefronts that the registers of a SIMD hold. (Two where four need more than 64 KB: 4,000 atoms,
+// 4 heads of 32, float32, reverse 598 us instead of 324. Four wherever they fit: 8 graphs of 700 atoms, 4 heads of 32, bf16, 64
+// buckets, reverse 64 us instead of 42. Without the half turn three: 54 us there.)
+constexpr int lds_pieces(int bytes) { return (bytes + 1279) / 1280; }   // LDS is given out in pieces of 1,280 bytes, 128 a compute unit
+int waves_that_fit(int64_t items, int simd, int wave_bytes, int extra) {
+  const double asked = (double)items / num_cus();
+  int best = 1;
+  double least = 0.0;
+  for (int nw = 1; nw <= 4; ++nw) {
+    const int lds = 128 / lds_pieces(wave_bytes * nw + extra), regs = 4 * simd / nw, fit = lds < regs ? lds : regs;
+    if (fit == 0) break;
+    const double time = (asked <= fit ? 1.0 : asked / fit + 0.5) / nw;
+    if (nw == 1 || time <= least) { best = nw; least = time; }
+  }
+  return best;
+}
+template <class... A>
+int32_t allow_lds(void (*kernel)(A...), int bytes) {
+  if (bytes > 64 * 1024) HGNN_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  return HGNN_OK;
 }
 
 // Long graphs: see attn_split.
 bool long_graphs(int64_t G, int64_t N) { return N >= 1024 * G; }
 
 // Workgroups per head of k_attn_dq (each leaves one partial of g_bias): every tile its own while they are few, then as many as run
-// at once, which registers and LDS (160 KB, given out in pieces of 1,280 bytes) decide. (40,041 atoms in 390 graphs, 8 heads,
+// at once, which registers and LDS decide. (40,041 atoms in 390 graphs, 8 heads,
 // bf16: 62 us; 72 with a tenth more, 67 with half as many more, 72 with a workgroup per tile.) In long graphs, where a
 // tile is a long chain, 4,096 and more are dealt out best.
 int64_t dq_per_head(int64_t max_tiles, int32_t N, int32_t G, int nh, int dh, int nb, bool bf16) {
@@ -1044,7 +1061,7 @@ int64_t dq_per_head(int64_t max_tiles, int32_t N, int32_t G, int nh, int dh, int
     const int dp = dh <= 32 ? 32 : dh <= 64 ? 64 : 128;
     const int lds = TABLE + (bf16 ? dp == 32 ? dq_wave_bytes<true, 32, 64>(nb) : dp == 64 ? dq_wave_bytes<true, 64, 64>(nb) : dq_wave_bytes<true, 128, 64>(nb)
                                   : dp == 32 ? dq_wave_bytes<false, 32, 64>(nb) : dp == 64 ? dq_wave_bytes<false, 64, 64>(nb) : dq_wave_bytes<false, 128, 64>(nb));
-    const int by_lds = 128 / ((lds + 1279) / 1280), by_registers = 4 * dq_waves(bf16, dp);
+    const int by_lds = 128 / lds_pieces(lds), by_registers = 4 * dq_waves(bf16, dp);
     at_once = (int64_t)num_cus() * (by_lds < by_registers ? by_lds : by_registers);
   }
   const int64_t most = at_once / nh;
@@ -1105,7 +1122,8 @@ bool attn_split(int64_t max_tiles, int heads, int64_t G, int64_t N, int rep) {
 template <bool BF, int DP, bool SPLIT>
 int32_t launch_fwd(hipStream_t st, AttnArgs a) {
   constexpr int WB = fwd_wave_bytes<BF, DP>(), extra = TABLE;
-  a.nw = SPLIT ? waves_that_fit(WB, extra) : 1;
+  a.nw = SPLIT ? waves_that_fit(a.plan.max_tiles * a.nh, DP == 128 ? 1 : DP == 32 ? 4 : BF ? 3 : 2, WB, extra) : 1;
+  HGNN_TRY(allow_lds(k_attn_fwd<BF, DP, SPLIT>, WB * a.nw + extra));
   k_attn_fwd<BF, DP, SPLIT><<<(unsigned)item_blocks(a.near, a.plan.max_tiles, a.nh), 64 * a.nw, WB * a.nw + extra, st>>>(a);
   HGNN_LAUNCH_CHECK("k_attn_fwd");
   return HGNN_OK;
@@ -1114,7 +1132,8 @@ int32_t launch_fwd(hipStream_t st, AttnArgs a) {
 template <bool BF, int DP, bool SPLIT, bool LONG>
 int32_t launch_dq(hipStream_t st, AttnArgs a) {
   const int wb = dq_wave_bytes<BF, DP, LONG ? 32 : 64>(a.nb), extra = TABLE;
-  a.nw = SPLIT ? waves_that_fit(wb, extra) : 1;
+  a.nw = SPLIT ? waves_that_fit((int64_t)a.per_head * a.nh, dq_waves(BF, DP), wb, extra) : 1;
+  HGNN_TRY(allow_lds(k_attn_dq<BF, DP, SPLIT, LONG>, wb * a.nw + extra));
   k_attn_dq<BF, DP, SPLIT, LONG><<<(unsigned)item_blocks(a.near, a.per_head, a.nh), 64 * a.nw, wb * a.nw + extra, st>>>(a);
   HGNN_LAUNCH_CHECK("k_attn_dq");
   return HGNN_OK;
@@ -1123,7 +1142,8 @@ int32_t launch_dq(hipStream_t st, AttnArgs a) {
 template <bool BF, int DP, bool SPLIT>
 int32_t launch_dkv(hipStream_t st, AttnArgs a) {
   constexpr int WB = TABLE + dkv_wave_bytes<BF, DP>();
-  a.nw = SPLIT ? waves_that_fit(WB, 0) : 1;
+  a.nw = SPLIT ? waves_that_fit(a.plan.max_tiles * a.nkv, dq_waves(BF, DP), WB, 0) : 1;
+  HGNN_TRY(allow_lds(k_attn_dkv<BF, DP, SPLIT>, WB * a.nw));
   k_attn_dkv<BF, DP, SPLIT><<<(unsigned)(item_blocks(a.near, a.plan.max_tiles, a.nkv) + a.nh), 64 * a.nw, WB * a.nw, st>>>(a);
   HGNN_LAUNCH_CHECK("k_attn_dkv");
   return HGNN_OK;
