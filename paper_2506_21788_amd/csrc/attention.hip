@@ -439,7 +439,7 @@ struct Where {
   const uint8_t* pairs;    // the graph's matrix
 };
 __device__ __forceinline__ Where tile_where(const AttnArgs& a, int t) {
-  const PairTile r = a.plan.tile[t];
+  const PairTile r = a.plan.tile[t < a.plan.max_tiles ? t : a.plan.max_tiles - 1];   // (also asked for before t is known to exist)
   Where w;
   w.lo = r.lo;
   w.n = r.n;
@@ -491,11 +491,12 @@ __global__ void __launch_bounds__(256, DP == 128 ? 1 : 2) k_attn_fwd(AttnArgs a)
   using T = typename Row<BF, DP>::T;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x & 63, wave = SPLIT ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0, g = lane >> 5;
-  const int ntiles = *a.plan.count;
   int t, h;
   item_of(a.near, blockIdx.x, a.nh, t, h);
-  if (t >= ntiles) return;   // uniform over the workgroup
+  const int ntiles = *a.plan.count;
   const Where w = tile_where(a, t);
+  asm volatile("" ::"s"(w.lo));   // both loads before either is waited for
+  if (t >= ntiles) return;   // uniform over the workgroup
   float* table = reinterpret_cast<float*>(smem);
   T* tk = reinterpret_cast<T*>(smem + TABLE + wave * fwd_wave_bytes<BF, DP>());
   T* tv = tk + 32 * Row<BF, DP>::PITCH;
@@ -896,12 +897,13 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k
     return;
   }
   const int lane = threadIdx.x & 63, wave = SPLIT ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0, g = lane >> 5;
-  const int ntiles = *a.plan.count;
   const unsigned item = blockIdx.x - a.nh;
   int t, hk;
   item_of(a.near, item, a.nkv, t, hk);
-  if (t >= ntiles) return;
+  const int ntiles = *a.plan.count;
   const Where w = tile_where(a, t);
+  asm volatile("" ::"s"(w.lo));   // (as in k_attn_fwd)
+  if (t >= ntiles) return;
   // (tables: wavefronts of one workgroup may be at different heads, so each has its own)
   const unsigned table_at = wave * TABLE;
   float* table = reinterpret_cast<float*>(smem + table_at);
