@@ -410,6 +410,7 @@ int32_t hgnn_pair_buckets(void* stream, int32_t N, int32_t G, const void* plan, 
  * Buckets have no gradient with respect to positions.
  * `saved` (NULL: no reverse pass follows) is written by _fwd and read by _bwd with the same out. plan: hgnn_pair_plan of this
  * batch; pairs: a pair matrix of it (its padding is not looked at).
+ * Outputs, saved and ws may alias nothing.
  * 1 <= nh <= 64, nkv divides nh, dh a multiple of 8 in 8..128, 1 <= nb <= 64, 1e-6 <= scale <= 1e6 (else BAD_SHAPE). N and G below 2^28, and
  * (N / 32 + min(N, G) + 64) nh below 2^26 (else OVERFLOW). Only enqueue work.
  * dtype HGNN_BF16 rounds p and ds to bfloat16 where they enter the products of g_q, g_k and g_v; out, g_bias and all softmax
@@ -434,7 +435,7 @@ int32_t hgnn_graph_attention_bwd(void* stream, int32_t N, int32_t G, int32_t nh,
  * rounded where it enters the product; gW and g_b carry no bf16 rounding.
  * `saved` (NULL: no reverse pass follows; of the queried size, which may be 0) is written by _fwd and read by _bwd of the same W.
  * _bwd writes g_x = r_x + g_z W^T (r_x NULL: none; g_x NULL: not wanted), gW and g_b (NULL: not wanted); the gradient of r is
- * g_y itself. r_x is what x has as a gradient from elsewhere. y may alias r, g_x may alias r_x.
+ * g_y itself. r_x is what x has as a gradient from elsewhere. y may alias r, g_x may alias r_x; no other aliasing.
  * M >= 0, 1 <= K, N <= 8192 (else BAD_SHAPE); M <= 2^26 (else OVERFLOW). Only enqueue work.
  * ------------------------------------------------------------------------------------------- */
 int32_t hgnn_dense_workspace_bytes(int32_t M, int32_t K, int32_t N, int32_t act, int32_t dtype, size_t* ws_bytes_host,
