@@ -431,8 +431,8 @@ int32_t hgnn_graph_attention_bwd(void* stream, int32_t N, int32_t G, int32_t nh,
  *   y = r + act(x W + b),  act: none, silu, or gelu z Phi(z) with the normal distribution's Phi (no approximation)
  * x is T [M,K], W T [K,N] row-major, b float32 [N] or NULL, r T [M,N] or NULL, y T [M,N]; gW and g_b are float32. With dtype
  * HGNN_F32 products are formed to float32 precision; with HGNN_BF16 x, W, r and y are bfloat16 in memory (hgnn_round_bf16 makes
- * such a copy of a float32 weight buffer, nearest even) and y and g_x are rounded once, g_x from a g_z = g_y act'(z) that is
- * rounded where it enters the product; gW and g_b carry no bf16 rounding.
+ * such a copy of a float32 weight buffer, nearest even) and y and g_x are rounded once;
+ * g_z = g_y act'(z) enters the products of g_x and gW as two bf16 terms (off by at most 2^-17 of it; exact without an activation), g_b as it is.
  * `saved` (NULL: no reverse pass follows; of the queried size, which may be 0) is written by _fwd and read by _bwd of the same W.
  * _bwd writes g_x = r_x + g_z W^T (r_x NULL: none; g_x NULL: not wanted), gW and g_b (NULL: not wanted); the gradient of r is
  * g_y itself. r_x is what x has as a gradient from elsewhere. y may alias r, g_x may alias r_x; no other aliasing.

@@ -8,8 +8,9 @@
 // the result through transposing reads; both give a lane the contraction places 4 g + 0..3 and 8 + 4 g + 0..3 of 16.
 // float32 operands are staged as three bf16 terms and take six partial products (devmath.h): 2.7 times the rate of the float32
 // matrix cores at their precision. The forward pass keeps act'(z) in float32, so that the reverse pass multiplies by it where
-// it stages g_z: no tensor g_z exists. In gW, a sum over all rows, a bf16 call takes g_z as two bf16 terms, as the one
-// rounding that g_z = g_y act'(z) would suffer has no business in a float32 result.
+// it stages g_z: no tensor g_z exists. A bf16 call takes g_z = g_y act'(z) as two bf16 terms (terms_of_gz), 16 bits: one would add a rounding
+// to g_x's own and leave gW, a float32 result, with 8. (A third in gW takes 7 % more time for the reverse pass of 40,041 x 256 -> 512; with two
+// its error there is 2.5e-6, that of a float32 sum over the rows 2.2e-6.)
 //
 // The two products with W (large calls): W is laid out once per call in the order in which the matrix cores take it (k_pack), a 1 KB fragment
 // per 32 columns and 16 places, in the one or three bf16 terms, and goes from the L2 to registers without LDS. Staged by every
@@ -119,14 +120,16 @@ __device__ __forceinline__ void split8(const float (&x)[8], u32x4_t (&o)[NT]) {
   }
 }
 
-// acc[i][j] += a[i] b[j] over the terms that count, smallest first (three terms each: the six products of devmath.h). Term by term
-// over all accumulators: a product that adds to the one before waits for it twice as long as it takes.
+// acc[i][j] += a[i] b[j] over the terms that count, smallest first (three terms each: the six products of devmath.h; else one operand is of
+// one term). Term by term over all accumulators: a product that adds to the one before waits for it twice as long as it takes.
 template <int NA, int NB, int WI, int WJ>
 __device__ __forceinline__ void mfma_terms(const bf16x8_t (&a)[WI][NA], const bf16x8_t (&b)[WJ][NB], f32x16_t (&acc)[WI][WJ]) {
-  constexpr int N = NA == 3 ? 6 : NB;
+  constexpr bool SIX = NA == 3 && NB == 3;
+  static_assert(SIX || NA == 1 || NB == 1);
+  constexpr int N = SIX ? 6 : NA > NB ? NA : NB;
 #pragma unroll
   for (int t = 0; t < N; ++t) {
-    const int ta = NA == 3 ? (t == 0 ? 2 : t == 1 || t == 3 ? 1 : 0) : 0, tb = NA == 3 ? (t == 2 ? 2 : t == 1 || t == 4 ? 1 : 0) : N - 1 - t;
+    const int ta = SIX ? (t == 0 ? 2 : t == 1 || t == 3 ? 1 : 0) : NA > 1 ? N - 1 - t : 0, tb = SIX ? (t == 2 ? 2 : t == 1 || t == 4 ? 1 : 0) : NB > 1 ? N - 1 - t : 0;
 #pragma unroll
     for (int i = 0; i < WI; ++i)
 #pragma unroll
@@ -448,10 +451,10 @@ __global__ void __launch_bounds__(256, 2) k_dense(DenseArgs a) {
 
 // The result's tile of 128 x 128 where operand b is packed; a: neighbours along the contraction. The slice of a is in LDS twice: one is
 // multiplied while the next is written, a barrier between.
-template <bool BF, int EPI, int NT, bool MUL>
+template <bool BF, int EPI, int NA, int NB, bool MUL>
 __global__ void __launch_bounds__(256, 2) k_dense_packed(DenseArgs a) {
-  constexpr int BC = BF ? 64 : 32, KS = BC / 16;
-  using SA = Slice<128, true, NT, BC>;
+  constexpr int BC = slice_places(NA, NB), KS = BC / 16;
+  using SA = Slice<128, true, NA, BC>;
   extern __shared__ __align__(16) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wi = wave >> 1, wj = wave & 1;
   int ti, tj, split;
@@ -465,12 +468,12 @@ __global__ void __launch_bounds__(256, 2) k_dense_packed(DenseArgs a) {
     if (q < a.J) get4(a.bias, q, bias, a.J - q);
   }
   const u32x4_t* pb = a.packed + ((size_t)(tj * 4 + wj * 2) * a.pkb) * 64 + lane;
-  bf16x8_t fb[KS][2][NT];
+  bf16x8_t fb[KS][2][NB];
   auto fetch_b = [&](int c, int s) {
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) fb[s][j][t] = __builtin_bit_cast(bf16x8_t, pb[((size_t)t * a.pterm + (size_t)j * a.pkb + c / 16 + s) * 64]);
+      for (int t = 0; t < NB; ++t) fb[s][j][t] = __builtin_bit_cast(bf16x8_t, pb[((size_t)t * a.pterm + (size_t)j * a.pkb + c / 16 + s) * 64]);
   };
   SA::template fetch<BF, MUL>(a.a, i0, 0, a.I, a.C, a.C, tid, va);
 #pragma unroll
@@ -483,13 +486,13 @@ __global__ void __launch_bounds__(256, 2) k_dense_packed(DenseArgs a) {
     const bool more = c + BC < a.C;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      bf16x8_t fa[2][NT];
+      bf16x8_t fa[2][NA];
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NA; ++t)
           fa[i][t] = *reinterpret_cast<const bf16x8_t*>(la + t * SA::PLANE + (wi * 64 + i * 32 + (lane & 31)) * SA::PITCH + 16 * s + 8 * (lane >> 5));
-      mfma_terms<NT, NT, 2, 2>(fa, fb[s], acc);
+      mfma_terms<NA, NB, 2, 2>(fa, fb[s], acc);
       if (more) fetch_b(c + BC, s);
     }
     if (more) {
@@ -761,15 +764,19 @@ size_t bwd_ws_bytes(int64_t M, int K, int N) {
   return w.nsplit > 1 ? (size_t)w.nsplit * ((size_t)K * N + N) * sizeof(float) : 0;
 }
 
+// Terms of an operand with factors, g_z = g_y act'(z). A bf16 call takes two (one: g_x off by 2.3e-3 instead of 1.7e-3 at 40,041 x 512 -> 256, in
+// the same time; 132 us instead of 140 for both directions at 8,400 x 866 -> 889, where the matrix cores are the limit).
+constexpr int terms_of_gz(bool bf16, bool mul) { return !bf16 ? 3 : mul ? 2 : 1; }
+
 template <bool BF, int EPI, bool MUL>
 int32_t launch_packed(hipStream_t st, DenseArgs a, const u32x4_t* packed) {
-  constexpr int NT = BF ? 1 : 3, lds_in = 2 * Slice<128, true, NT, BF ? 64 : 32>::BYTES, lds_out = 4 * 32 * (64 + 4) * 4;
+  constexpr int NA = terms_of_gz(BF, MUL), NB = BF ? 1 : 3, lds_in = 2 * Slice<128, true, NA, slice_places(NA, NB)>::BYTES, lds_out = 4 * 32 * (64 + 4) * 4;
   const Packed p = packed_of(a.C, a.J, BF);
   a.packed = packed; a.pkb = p.kb; a.pterm = p.term;
   a.ti = (a.I + 127) / 128;
   a.tj = (a.J + 127) / 128;
   const int64_t n = (int64_t)a.ti * a.tj;
-  k_dense_packed<BF, EPI, NT, MUL><<<(unsigned)((n + 7) / 8 * 8), 256, lds_in > lds_out ? lds_in : lds_out, st>>>(a);
+  k_dense_packed<BF, EPI, NA, NB, MUL><<<(unsigned)((n + 7) / 8 * 8), 256, lds_in > lds_out ? lds_in : lds_out, st>>>(a);
   HGNN_LAUNCH_CHECK("k_dense_packed");
   return HGNN_OK;
 }
@@ -805,7 +812,7 @@ int32_t run_bwd(hipStream_t st, int M, int K, int N, const void* x, const void* 
     a.b = {W, nullptr, N};
     a.res = r_x; a.out = g_x; a.nsplit = 1; a.per_split = N;
     if (wt) HGNN_TRY((launch_packed<BF, EPI_GX, MUL>(st, a, wt)));
-    else HGNN_TRY((launch_size<BF, EPI_GX, true, true, BF ? 1 : 3, BF ? 1 : 3, MUL, false>(st, a, tile_size(M, K, 1))));
+    else HGNN_TRY((launch_size<BF, EPI_GX, true, true, terms_of_gz(BF, MUL), BF ? 1 : 3, MUL, false>(st, a, tile_size(M, K, 1))));
   }
   const WSplit w = weight_split(M, K, N);
   DenseArgs a{};
@@ -816,7 +823,7 @@ int32_t run_bwd(hipStream_t st, int M, int K, int N, const void* x, const void* 
   const int64_t n = (int64_t)K * N;
   a.partial = w.nsplit > 1 ? ws : gW;
   a.colsum = g_b ? (w.nsplit > 1 ? ws + (size_t)w.nsplit * n : g_b) : nullptr;
-  HGNN_TRY((launch_size<BF, EPI_GW, false, false, BF ? 1 : 3, BF ? (MUL ? 2 : 1) : 3, false, MUL>(st, a, w.size)));
+  HGNN_TRY((launch_size<BF, EPI_GW, false, false, BF ? 1 : 3, terms_of_gz(BF, MUL), false, MUL>(st, a, w.size)));
   if (w.nsplit > 1) {
     k_dense_reduce<<<(unsigned)((n + N + 255) / 256), 256, 0, st>>>(a.partial, a.colsum, w.nsplit, n, N, gW, g_b);
     HGNN_LAUNCH_CHECK("k_dense_reduce");
