@@ -430,7 +430,8 @@ int32_t hgnn_graph_attention_bwd(void* stream, int32_t N, int32_t G, int32_t nh,
  * Dense product with bias, activation and residual in its epilogue, over M rows (atoms):
  *   y = r + act(x W + b),  act: none, silu, or gelu z Phi(z) with the normal distribution's Phi (no approximation)
  * x is T [M,K], W T [K,N] row-major, b float32 [N] or NULL, r T [M,N] or NULL, y T [M,N]; gW and g_b are float32. With dtype
- * HGNN_F32 products are formed to float32 precision; with HGNN_BF16 x, W, r and y are bfloat16 in memory (hgnn_round_bf16 makes
+ * HGNN_F32 products are formed to float32 precision (infinite and largest operands included, which are slow; of operands below 2^-110 in
+ * magnitude what is smaller than 2^-134 is lost); with HGNN_BF16 x, W, r and y are bfloat16 in memory (hgnn_round_bf16 makes
  * such a copy of a float32 weight buffer, nearest even) and y and g_x are rounded once;
  * g_z = g_y act'(z) enters the products of g_x and gW as two bf16 terms (off by at most 2^-17 of it; exact without an activation), g_b as it is.
  * `saved` (NULL: no reverse pass follows; of the queried size, which may be 0) is written by _fwd and read by _bwd of the same W.

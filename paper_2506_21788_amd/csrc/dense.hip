@@ -224,6 +224,41 @@ struct Slice {
   }
 };
 
+// Operands of several terms only reach to the largest bf16 number, 3.39e38: a larger one, and an infinite one, has an infinite first
+// term, and that is no number with a remainder of the other operand that is zero or of the other sign, or with its own. So where a
+// wavefront's 32 x 32 results are not all finite, those that are not are formed again from the operands themselves, on the float32
+// matrix cores: what the definition makes infinite is infinite, what it makes finite is finite. Results (i0 .., j0 ..), contraction places
+// c .. c + run - 1 of every `step` up to c1. Such values are slow (40,041 x 256 -> 512 bf16 with silu, both
+// directions: one infinite operand 0.74 ms, nothing but NaN 1.9 ms instead of 0.13); all others pay 16 operations for the test.
+template <bool BF, bool KC, bool MUL>
+__device__ __forceinline__ float value_at(const Operand& o, int e, int ne, int k, int nk) {
+  if (e >= ne || k >= nk) return 0.f;
+  const size_t at = KC ? (size_t)e * o.ld + k : (size_t)k * o.ld + e;
+  float x;
+  if constexpr (BF) x = __uint_as_float((unsigned)static_cast<const unsigned short*>(o.p)[at] << 16);
+  else x = static_cast<const float*>(o.p)[at];
+  if constexpr (MUL) x *= o.mul[at];
+  return x;
+}
+template <bool BF, bool AKC, bool BKC, int NA, int NB, bool AMUL, bool BMUL>
+__device__ __forceinline__ void form_again(const DenseArgs& a, int i0, int j0, int c, int run, int step, int c1, int lane, f32x16_t& acc) {
+  if constexpr (NA > 1 || NB > 1) {   // (single terms are the operands themselves)
+    float z = 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) z = fmaf(acc[v], 0.f, z);
+    if (__all(z == 0.f)) return;
+    f32x16_t s = {};
+#pragma unroll 1
+    for (; c < c1; c += step)
+#pragma unroll 1
+      for (int k = c; k < c + run; k += 2)
+        s = __builtin_amdgcn_mfma_f32_32x32x2f32(value_at<BF, AKC, AMUL>(a.a, i0 + (lane & 31), a.I, k + (lane >> 5), c1),
+                                                 value_at<BF, BKC, BMUL>(a.b, j0 + (lane & 31), a.J, k + (lane >> 5), c1), s, 0, 0, 0);
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[v] = fabsf(acc[v]) < __builtin_inff() ? acc[v] : s[v];
+  }
+}
+
 // act(z) and act'(z)
 __device__ __forceinline__ void activate(int act, float z, float& y, float& dy) {
   if (act == HGNN_ACT_SILU) {
@@ -412,6 +447,11 @@ __global__ void __launch_bounds__(256, 2) k_dense(DenseArgs a) {
       mfma_terms<NA, NB, WI, WJ>(fa, fb, acc);
     }
   }
+#pragma unroll
+  for (int i = 0; i < WI; ++i)
+#pragma unroll
+    for (int j = 0; j < WJ; ++j)
+      form_again<BF, AKC, BKC, NA, NB, AMUL, BMUL>(a, i0 + wi * (EI / 2) + i * 32, j0 + wj * (EJ / 2) + j * 32, c0, BC, BC, c1, lane, acc[i][j]);
   if constexpr (EPI == EPI_GW) {
     if (sums) {   // the threads that took the same columns, in order (a column's chunks: threads q, q + EJ/8, ...)
       static_assert(!BKC, "the rows of the slice are contraction places");
@@ -501,6 +541,11 @@ __global__ void __launch_bounds__(256, 2) k_dense_packed(DenseArgs a) {
     }
     __syncthreads();
   }
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)   // (W [K][N] is operand b of y, and of g_x by its rows)
+      form_again<BF, true, EPI == EPI_GX, NA, NB, MUL, false>(a, i0 + wi * 64 + i * 32, j0 + wj * 64 + j * 32, 0, BC, BC, a.C, lane, acc[i][j]);
   store_tile<BF, EPI, 128, 128>(a, acc, bias, i0, j0, wave, lane, smem);
 }
 
@@ -594,6 +639,7 @@ __global__ void __launch_bounds__(256) k_dense_small(DenseArgs a) {
       for (int k = 0; k < 8; ++k) cs += y[k];
     }
   }
+  form_again<BF, AKC, BKC, NA, NB, AMUL, BMUL>(a, ti * 32, tj * 32, c0 + wave * 16, 16, 64, c1, lane, acc[0][0]);
 #pragma unroll
   for (int v = 0; v < 16; ++v) join[wave][v][lane] = acc[0][0][v];
   if constexpr (EPI == EPI_GW) cjoin[wave][lane] = cs;
