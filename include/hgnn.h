@@ -26,7 +26,8 @@
  *  - dtype selects the GEMM operand type: HGNN_F32 (fp32 matrix cores) or HGNN_BF16 (operands rounded
  *    to bf16 on load, fp32 accumulation). Activations, aggregation, biases and SiLU stay fp32.
  *  - Gradient outputs are overwritten, not accumulated, unless said otherwise.
- *  - Results are deterministic: no two threads add to one floating-point word, all reductions in a fixed order.
+ *  - Results are deterministic: all floating-point sums are formed in a fixed order, and nothing adds to floating-point memory atomically
+ *    (hgnn_graph_attention_bwd lets two lanes of a wavefront add to one word of its LDS, one after the other).
  */
 #ifndef HGNN_H
 #define HGNN_H

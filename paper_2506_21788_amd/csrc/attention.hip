@@ -22,8 +22,8 @@
 // 8 heads of 32 on 2, bf16, take 47 us forward (vector units 65 % busy) and 62 + 56 us in reverse (k_attn_dq: LDS 55, vector units 40 %).
 //
 // The sums of the reverse pass are split in two kernels (one owns queries, one keys) rather than added with atomics, so that
-// their order is fixed: the scores are formed twice. g_bias is collected in LDS, a column per lane and bucket (no two lanes
-// share a word), over all tiles that a wavefront takes, and then added up over the wavefronts in order.
+// their order is fixed: the scores are formed twice. g_bias is collected in LDS, a column per lane and bucket (in long graphs lanes i and
+// i + 32 share one and add in turn), over all tiles that a wavefront takes, and then added up over the wavefronts in order.
 //
 // A pair that is left out must not be touched by what its atoms hold, but a matrix product multiplies it by zero, and 0 * inf is
 // no number. So a wavefront whose result is not finite forms its rows again, pair by pair over the pairs that count.
@@ -783,9 +783,11 @@ __global__ void __launch_bounds__(256, dq_waves(BF, DP)) k_attn_dq(AttnArgs a) {
           for (int i = 0; i < 16; ++i) {
             const unsigned e = entry_of<7>(bc, i);
             far_sum += e == last ? ds[i] : 0.f;
-            if (__any(e < last)) {   // (the two lanes of a column, one after the other)
+            if (__any(e < last)) {   // (the two lanes of a column, one after the other: the fences keep both turns apart, and from the next place's)
               if (e < last && g == 0) __hip_atomic_fetch_add(&lds<float>(e + col), ds[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+              lds_order();
               if (e < last && g == 1) __hip_atomic_fetch_add(&lds<float>(e + col), ds[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+              lds_order();
             }
           }
         } else {

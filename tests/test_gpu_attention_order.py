@@ -1,0 +1,76 @@
+"""Attention where a workgroup takes several tiles, where heads lie far apart and where sums are taken in turns; the terms of its weights (needs a GPU)."""
+import numpy as np
+import pytest
+
+from block_util import U32, dev, empty
+from oracle import block as ob
+from test_gpu_attention import _check, _problem, _run
+
+pytestmark = pytest.mark.gpu
+
+
+def _common(P, rare, seed=0):
+    """Most pairs into the last bucket, as in a large structure; the first rows keep a mixture."""
+    rng = np.random.default_rng(seed)
+    where, pitch = ob.pair_layout(P["off"])
+    for k in range(P["G"]):
+        n = int(P["off"][k + 1] - P["off"][k])
+        m = P["pairs"][where[k]:where[k + 1]].reshape(n, pitch[k])
+        common = (rng.random((n, n)) > rare) & (m[:, :n] < P["nb"])
+        common[:40] = False
+        m[:, :n][common] = P["nb"] - 1
+    return P
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_long_graphs_with_more_tiles_than_workgroups(dtype):
+    """64 heads have 64 workgroups each in the pass over queries, for 106 tiles: tables, sums and joins go on from tile to tile."""
+    _check(_common(_problem([1100, 1029, 1100], 64, 8, 8, 6, dtype, left_out=0.02), 0.01))
+
+
+@pytest.mark.parametrize("dtype,heads,kv,d", [("f32", 4, 2, 128), ("f32", 8, 4, 64), ("bf16", 4, 4, 128)])
+@pytest.mark.parametrize("n", [1000, 1100])
+def test_heads_far_apart(n, dtype, heads, kv, d):
+    """Keys and values of a graph past 1 MB: its heads are dealt to different parts of the chip."""
+    assert 2 * n * kv * d * (2 if dtype == "bf16" else 4) > 2e6
+    P = _problem([n], heads, kv, d, 12, dtype, left_out=0.02)
+    _check(_common(P, 0.01) if n > 1024 else P)
+
+
+@pytest.mark.parametrize("drop_far", [False, True])
+def test_sums_in_turn_repeat_themselves(drop_far):
+    """Two pairs of one row that add to one word of LDS (16 keys apart, in one bucket): the same bits every time, and the right sum. drop_far:
+    what is beyond the last boundary takes no part."""
+    P = _problem([1090], 2, 1, 32, 9, "bf16", holes=False)
+    m = P["pairs"][:1090 * 1120].reshape(1090, 1120)
+    m[:, :1090] = 255 if drop_far else 8
+    i = np.arange(1090)
+    for step in (0, 16, 5):                     # in every row three near pairs, two of them a half tile apart
+        m[i, (i + step) % 1090] = 3
+    got = _check(P)
+    for _ in range(3):
+        assert all(np.array_equal(a, b) for a, b in zip(_run(P), got))
+
+
+def test_weights_of_the_output_enter_whole():
+    """All values of a graph are 1 and all of g_out too: dP = D = d exactly if the weights in the output are those of the row's sum, and then
+    g_bias = 0. With two bf16 terms of each weight the output falls short of 1 by some 2^-17 and g_bias shows it."""
+    n, G, d, nb = 5, 60, 8, 12
+    P = _problem([n] * G, 1, 1, d, nb, "bf16", holes=False)
+    P["qkv"][:, :2], P["qkv"][:, 2], P["g"][:] = 0.0, 1.0, 1.0
+    got = _run(P)
+    allowed, short = np.zeros(nb), np.zeros(nb)
+    where, pitch = ob.pair_layout(P["off"])
+    for k in range(G):
+        m = P["pairs"][where[k]:where[k + 1]].reshape(n, pitch[k])[:, :n].astype(int)
+        s = P["bias"][0][m]
+        w = np.exp(s - s.max(1, keepdims=True)).astype(np.float32)
+        p = w.astype(np.float64) / w.astype(np.float64).sum(1, keepdims=True)
+        cut = lambda x: (x.view(np.uint32) & 0xffff0000).view(np.float32)  # noqa: E731
+        two = cut(w) + cut(w - cut(w))
+        delta = 1.0 - two.astype(np.float64).sum(1, keepdims=True) / w.astype(np.float64).sum(1, keepdims=True)
+        # the products of n weights in three terms, their sum, the quotient, D's sum over d equal terms
+        allowed += np.bincount(m.ravel(), weights=(p * d * (4 * n + 8) * U32).ravel(), minlength=nb)
+        short += np.bincount(m.ravel(), weights=(p * d * delta).ravel(), minlength=nb)
+    assert (short > 1.5 * allowed).all(), "a weight of two terms would not show"
+    assert (np.abs(got[2][0]) <= allowed).all(), np.abs(got[2][0] / allowed).max()
