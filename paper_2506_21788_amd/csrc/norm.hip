@@ -19,6 +19,7 @@ namespace {
 
 struct NormArgs {
   int N, H;
+  int first;                 // first row of a forward launch
   int layer, gate;
   float eps;
   const float *x, *P;
@@ -91,7 +92,7 @@ template <class T, int LPR, int V, int NC>
 __global__ void __launch_bounds__(256) k_norm_fwd(NormArgs a) {
   constexpr int RPW = 64 / LPR;
   const int lane = threadIdx.x & 63, sub = lane / LPR;
-  const long row = ((long)blockIdx.x * 4 + (threadIdx.x >> 6)) * RPW + sub;
+  const long row = a.first + ((long)blockIdx.x * 4 + (threadIdx.x >> 6)) * RPW + sub;
   const int col = (lane % LPR) * V;
   if (row >= a.N) return;
   const long at = row * a.H + col;
@@ -299,11 +300,20 @@ int norm_bwd_groups(int N, int H) {
 
 // the widest access that every row's start is aligned to, and the lanes and chunks that hold a row
 template <class T, bool FWD>
-void launch_norm(hipStream_t st, const NormArgs& a, int groups) {
+void launch_norm(hipStream_t st, NormArgs a, int groups) {
+  constexpr int MOST = (1 << 24) - 1;   // workgroups of a launch, which has to have fewer than 2^32 threads
 #define HGNN_NORM(LPR, V, NC)                                                                                       \
   do {                                                                                                              \
-    if (FWD) k_norm_fwd<T, LPR, V, NC><<<(unsigned)((a.N + 4 * (64 / LPR) - 1) / (4 * (64 / LPR))), 256, 0, st>>>(a); \
-    else k_norm_bwd<T, LPR, V, NC><<<groups, 256, 0, st>>>(a);                                                      \
+    constexpr int ROWS = 4 * (64 / LPR);                                                                            \
+    if (FWD) {                                                                                                      \
+      for (int64_t left = a.N; left > 0; left -= (int64_t)MOST * ROWS) {                                            \
+        const int64_t n = (left + ROWS - 1) / ROWS;                                                                 \
+        a.first = (int)(a.N - left);                                                                                \
+        k_norm_fwd<T, LPR, V, NC><<<(unsigned)(n < MOST ? n : MOST), 256, 0, st>>>(a);                              \
+      }                                                                                                             \
+    } else {                                                                                                        \
+      k_norm_bwd<T, LPR, V, NC><<<groups, 256, 0, st>>>(a);                                                         \
+    }                                                                                                               \
     return;                                                                                                         \
   } while (0)
   const int H = a.H;
@@ -329,7 +339,7 @@ void launch_norm(hipStream_t st, const NormArgs& a, int groups) {
 
 int32_t check_norm(int32_t N, int32_t H, int32_t norm, int32_t gate, int32_t dtype) {
   HGNN_REQUIRE(N >= 0, HGNN_ERR_BAD_SHAPE, "negative N");
-  HGNN_REQUIRE(N < (1 << 26), HGNN_ERR_OVERFLOW, "block_norm: N must be below 2^26 (a launch has fewer than 2^32 threads)");
+  HGNN_REQUIRE(N < (1 << 26), HGNN_ERR_OVERFLOW, "block_norm: N must be below 2^26");
   HGNN_REQUIRE(H >= 1 && H <= 1024, HGNN_ERR_BAD_SHAPE, "block_norm: H must be in 1..1024 (got %d)", H);
   HGNN_REQUIRE(norm == HGNN_NORM_RMS || norm == HGNN_NORM_LAYER, HGNN_ERR_BAD_SHAPE, "unknown norm %d", norm);
   HGNN_REQUIRE(gate == HGNN_GATE_NONE || gate == HGNN_GATE_ATOM || gate == HGNN_GATE_CHANNEL, HGNN_ERR_BAD_SHAPE, "unknown gate %d", gate);
