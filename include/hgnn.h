@@ -448,7 +448,7 @@ int32_t hgnn_dense_fwd(void* stream, int32_t M, int32_t K, int32_t N, int32_t ac
 int32_t hgnn_dense_bwd(void* stream, int32_t M, int32_t K, int32_t N, int32_t act, int32_t dtype, const void* x, const void* W,
                        const void* saved, size_t saved_bytes, const void* g_y, const void* r_x /*T [M,K] or NULL*/,
                        void* g_x /*out or NULL*/, float* gW /*out [K,N]*/, float* g_b /*out [N] or NULL*/, void* ws, size_t ws_bytes);
-int32_t hgnn_round_bf16(void* stream, int64_t n, const float* src, void* dst /*out, bf16*/);
+int32_t hgnn_round_bf16(void* stream, int64_t n /*0 .. 2^41 - 1, else BAD_SHAPE, OVERFLOW*/, const float* src, void* dst /*out, bf16*/);
 
 /* ---------------------------------------------------------------------------------------------
  * AdamW update of a flat float32 parameter buffer (paper, training setup: the optimiser is AdamW, learning rate 1e-3;

@@ -945,12 +945,16 @@ extern "C" int32_t hgnn_dense_bwd(void* stream, int32_t M, int32_t K, int32_t N,
 
 extern "C" int32_t hgnn_round_bf16(void* stream, int64_t n, const float* src, void* dst) {
   HGNN_REQUIRE(n >= 0, HGNN_ERR_BAD_SHAPE, "negative count");
-  HGNN_REQUIRE(n < (int64_t)INT_MAX * 1024, HGNN_ERR_OVERFLOW, "round_bf16: too many values for one launch");
+  HGNN_REQUIRE(n < (int64_t)1 << 41, HGNN_ERR_OVERFLOW, "round_bf16: n must be below 2^41");
   if (n == 0) return HGNN_OK;
   HGNN_REQUIRE(src && dst, HGNN_ERR_NULLPTR, "round_bf16: null pointer");
   hipStream_t st = static_cast<hipStream_t>(stream);
   ProfScope ps(PT_MISC, st);
-  k_round_bf16<<<(unsigned)((n + 2047) / 2048), 256, 0, st>>>(n, src, static_cast<unsigned short*>(dst));
-  HGNN_LAUNCH_CHECK("k_round_bf16");
+  constexpr int64_t MOST = (int64_t)((1 << 24) - 1) * 2048;   // values of a launch, which has to have fewer than 2^32 threads
+  for (int64_t at = 0; at < n; at += MOST) {
+    const int64_t k = n - at < MOST ? n - at : MOST;
+    k_round_bf16<<<(unsigned)((k + 2047) / 2048), 256, 0, st>>>(k, src + at, static_cast<unsigned short*>(dst) + at);
+    HGNN_LAUNCH_CHECK("k_round_bf16");
+  }
   return HGNN_OK;
 }
