@@ -27,6 +27,12 @@ class AttentionConfig:
     act: str = "silu"               # or "gelu", "none"
     eps: float = 1e-5
 
+    def __post_init__(self):
+        # (squares are compared, and searched: a negative or falling boundary would give wrong buckets without an error)
+        e = (0.0, *self.edges, float("inf"))
+        assert all(a <= b for a, b in zip(e, e[1:])), f"boundaries must ascend from 0: {self.edges}"
+        assert self.kv_heads is None or self.kv_heads >= 1, "kv_heads: None or at least 1"
+
     @property
     def kv(self):
         return self.kv_heads or self.heads
