@@ -1216,7 +1216,7 @@ extern "C" int32_t hgnn_graph_attention_fwd(void* stream, int32_t N, int32_t G, 
   a.stat = saved ? s.stat : nullptr;
   a.o32 = saved ? s.o32 : nullptr;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  ProfScope ps(PT_MISC, st);
+  ProfScope ps(PT_ATTENTION, st);
   return dtype == HGNN_BF16 ? run_attn<true>(st, a, true) : run_attn<false>(st, a, true);
 }
 
@@ -1246,6 +1246,6 @@ extern "C" int32_t hgnn_graph_attention_bwd(void* stream, int32_t N, int32_t G, 
   a.scale = scale; a.c = scale * LOG2E; a.inv = 1.0f / scale;
   a.pairs = pairs; a.qkv = qkv; a.bias = bias; a.out = const_cast<void*>(out); a.stat = s.stat; a.o32 = s.o32;
   a.g_out = g_out; a.g_qkv = g_qkv; a.delta = w.delta; a.partial = w.partial; a.g_bias = g_bias;
-  ProfScope ps(PT_MISC, st);
+  ProfScope ps(PT_ATTENTION, st);
   return dtype == HGNN_BF16 ? run_attn<true>(st, a, false) : run_attn<false>(st, a, false);
 }

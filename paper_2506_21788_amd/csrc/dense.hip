@@ -911,7 +911,7 @@ extern "C" int32_t hgnn_dense_fwd(void* stream, int32_t M, int32_t K, int32_t N,
   a.nsplit = 1; a.per_split = K;
   hipStream_t st = static_cast<hipStream_t>(stream);
   u32x4_t *pk = static_cast<u32x4_t*>(ws), *wt = saved ? s.wt : nullptr;
-  ProfScope ps(PT_MISC, st);
+  ProfScope ps(PT_DENSE, st);
   return dtype == HGNN_BF16 ? run_fwd<true>(st, a, W, pk, wt) : run_fwd<false>(st, a, W, pk, wt);
 }
 
@@ -935,7 +935,7 @@ extern "C" int32_t hgnn_dense_bwd(void* stream, int32_t M, int32_t K, int32_t N,
   HGNN_REQUIRE(wneed == 0 || ws, HGNN_ERR_NULLPTR, "dense_bwd: null workspace");
   HGNN_REQUIRE(ws_bytes >= wneed, HGNN_ERR_WORKSPACE_TOO_SMALL, "dense workspace: need %zu bytes, got %zu", wneed, ws_bytes);
   float* w = static_cast<float*>(ws);
-  ProfScope ps(PT_MISC, st);
+  ProfScope ps(PT_DENSE, st);
   if (dtype == HGNN_BF16)
     return act == HGNN_ACT_NONE ? run_bwd<true, false>(st, M, K, N, x, W, s.wt, nullptr, g_y, r_x, g_x, gW, g_b, w)
                                 : run_bwd<true, true>(st, M, K, N, x, W, s.wt, s.dact, g_y, r_x, g_x, gW, g_b, w);
@@ -949,7 +949,7 @@ extern "C" int32_t hgnn_round_bf16(void* stream, int64_t n, const float* src, vo
   if (n == 0) return HGNN_OK;
   HGNN_REQUIRE(src && dst, HGNN_ERR_NULLPTR, "round_bf16: null pointer");
   hipStream_t st = static_cast<hipStream_t>(stream);
-  ProfScope ps(PT_MISC, st);
+  ProfScope ps(PT_DENSE, st);
   constexpr int64_t MOST = (int64_t)((1 << 24) - 1) * 2048;   // values of a launch, which has to have fewer than 2^32 threads
   for (int64_t at = 0; at < n; at += MOST) {
     const int64_t k = n - at < MOST ? n - at : MOST;

@@ -376,7 +376,7 @@ extern "C" int32_t hgnn_block_norm_fwd(void* stream, int32_t N, int32_t H, int32
   a.N = N; a.H = H; a.layer = norm == HGNN_NORM_LAYER; a.gate = gate; a.eps = eps;
   a.x = x; a.b = b; a.z = z; a.P = P; a.x_out = x_out; a.y = y; a.saved = static_cast<float*>(saved);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  ProfScope ps(PT_MISC, st);
+  ProfScope ps(PT_BLOCK_NORM, st);
   if (dtype == HGNN_BF16) launch_norm<unsigned short, true>(st, a, 0);
   else launch_norm<float, true>(st, a, 0);
   HGNN_LAUNCH_CHECK("k_norm_fwd");
@@ -405,7 +405,7 @@ extern "C" int32_t hgnn_block_norm_bwd(void* stream, int32_t N, int32_t H, int32
   a.x = x_out; a.b = b; a.z = z; a.P = P; a.saved = const_cast<float*>(static_cast<const float*>(saved));
   a.g_x_out = g_x_out; a.g_y = g_y; a.g_x = g_x; a.g_b = g_b; a.g_z = g_z; a.gP = gP; a.partial = static_cast<float*>(ws);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  ProfScope ps(PT_MISC, st);
+  ProfScope ps(PT_BLOCK_NORM, st);
   if (N > 0) {
     if (dtype == HGNN_BF16) launch_norm<unsigned short, false>(st, a, groups);
     else launch_norm<float, false>(st, a, groups);

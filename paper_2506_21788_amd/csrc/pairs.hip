@@ -373,7 +373,7 @@ extern "C" int32_t hgnn_pair_plan(void* stream, int32_t N, int32_t G, const int3
   MailSlot mail;
   HGNN_TRY(mail.take(st));
   {
-    ProfScope ps(PT_MISC, st);
+    ProfScope ps(PT_PAIRS, st);
     k_pair_plan<<<1, 1024, 0, st>>>(N, G, graph_off, v, mail.dev());
     HGNN_LAUNCH_CHECK("k_pair_plan");
   }
@@ -395,7 +395,7 @@ extern "C" int32_t hgnn_pair_buckets(void* stream, int32_t N, int32_t G, const v
   HGNN_REQUIRE(plan_bytes >= a.plan.bytes, HGNN_ERR_WORKSPACE_TOO_SMALL, "pair plan: need %zu bytes, got %zu", a.plan.bytes, plan_bytes);
   a.nedge = nedge; a.drop_far = drop_far; a.pos = pos; a.cell = cell; a.edge2 = edge2; a.pbc = pbc; a.pairs = pairs;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  ProfScope ps(PT_MISC, st);
+  ProfScope ps(PT_PAIRS, st);
   constexpr int64_t MOST = (1 << 22) - 1;   // tiles of a launch, which has to have fewer than 2^32 threads
   for (a.first = 0; a.first < a.plan.max_tiles; a.first += MOST) {
     const int64_t left = a.plan.max_tiles - a.first;

@@ -35,6 +35,10 @@ enum ProfTag : int {
   PT_TO_FRAG,           // fragment path (widths other than 64 / 128 / 256): row-major -> fragment conversions of atom tensors
   PT_GEMM_ROWS,         // small batches: the chain of products that also finishes the forward sums
   PT_GEMM_REDUCE,       // small batches: the last product of a reverse pass and its reductions of split partials
+  PT_BLOCK_NORM,        // attention block: norms, gate, residual
+  PT_PAIRS,             // attention block: pair plan and distance buckets
+  PT_ATTENTION,         // attention block: attention over the atoms of each graph
+  PT_DENSE,             // attention block: dense products, bf16 copies of weights
   PT_COUNT
 };
 

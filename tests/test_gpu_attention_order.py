@@ -74,3 +74,39 @@ def test_weights_of_the_output_enter_whole():
         short += np.bincount(m.ravel(), weights=(p * d * delta).ravel(), minlength=nb)
     assert (short > 1.5 * allowed).all(), "a weight of two terms would not show"
     assert (np.abs(got[2][0]) <= allowed).all(), np.abs(got[2][0] / allowed).max()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_captured_where_a_workgroup_takes_more_than_64_kb(dtype):
+    import torch
+    from paper_2506_21788_amd import binding as B
+    P = _problem([400], 4, 1, 128, 64, dtype)
+    N, code = P["N"], B.BF16 if dtype == "bf16" else B.F32
+    args = (N, 1, 4, 1, 128, 64, code, P["scale"])
+    plan = torch.empty(B.pair_plan_workspace_bytes(N, 1), dtype=torch.uint8, device="cuda")
+    B.pair_plan(N, 1, dev(P["off"], "i32"), plan)
+    ws_b, saved_b = B.graph_attention_workspace_bytes(*args[:7])
+    ws, saved = (torch.empty(k, dtype=torch.uint8, device="cuda") for k in (ws_b, saved_b))
+    pairs, qkv, bias, g = dev(P["pairs"], "u8"), dev(P["qkv"], dtype), dev(P["bias"]), dev(P["g"], dtype)
+    res = [empty((N, 4, 128), dtype), empty((N, 6, 128), dtype), empty((4, 64))]
+
+    def both():
+        B.graph_attention_fwd(*args, plan, pairs, qkv, bias, res[0], saved)
+        B.graph_attention_bwd(*args, plan, pairs, qkv, bias, res[0], saved, g, res[1], res[2], ws)
+
+    both()
+    torch.cuda.synchronize()
+    want = [r.clone() for r in res]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for _ in range(3):
+        for r in res:
+            r.fill_(float("nan"))
+        ws.fill_(255)
+        saved.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, w) for a, w in zip(res, want))
+        both()
+        torch.cuda.synchronize()

@@ -103,3 +103,26 @@ def test_replays_write_every_gradient_of_the_blocks(dtype):
         path.forward()
         path.backward(gE, gF)
         torch.cuda.synchronize()
+
+
+def test_profile_shows_the_blocks_by_class():
+    """One launch scope per call: of a step with two gated blocks 6 norms each, 2 attention calls, 10 dense products and a copy of the weights."""
+    import torch
+    from paper_2506_21788_amd import binding as B
+    P = _problem(64, "bf16", 35, _config())
+    path = gpu_hotpath(P)
+    gE, gF = torch.as_tensor(P["gE"]).cuda(), torch.as_tensor(P["gF"]).cuda()
+
+    def count(work):
+        torch.cuda.synchronize()
+        B.profile_begin((1 << B.profile_num_tags()) - 1)
+        work()
+        B.profile_end()
+        return {B.profile_tag_name(t): B.profile_read(t) for t in range(B.profile_num_tags())}
+
+    got = count(path.build_graph)
+    assert got["pairs"][0] == 2 and got["pairs"][1] > 0.0
+    path.step(gE, gF)
+    got = count(lambda: (path.forward(), path.backward(gE, gF)))
+    assert [got[k][0] for k in ("block_norm", "attention", "dense", "pairs")] == [12, 4, 22, 0]
+    assert all(got[k][1] > 0.0 for k in ("block_norm", "attention", "dense"))
