@@ -779,10 +779,11 @@ __global__ void __launch_bounds__(256, dq_waves(BF, DP)) k_attn_dq(AttnArgs a) {
       if constexpr (LONG) {
         const unsigned last = (a.nb - 1) * 128u;
         if (far) {
+          float tile = 0.f;   // (the tile's first: thousands of terms in one chain would lose places)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const unsigned e = entry_of<7>(bc, i);
-            far_sum += e == last ? ds[i] : 0.f;
+            tile += e == last ? ds[i] : 0.f;
             if (__any(e < last)) {   // (the two lanes of a column, one after the other: the fences keep both turns apart, and from the next place's)
               if (e < last && g == 0) __hip_atomic_fetch_add(&lds<float>(e + col), ds[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
               lds_order();
@@ -790,6 +791,7 @@ __global__ void __launch_bounds__(256, dq_waves(BF, DP)) k_attn_dq(AttnArgs a) {
               lds_order();
             }
           }
+          far_sum += tile;
         } else {
           for (int half = 0; half < 2; ++half) {
             if (g == half) {
@@ -862,12 +864,13 @@ __global__ void __launch_bounds__(256, dq_waves(BF, DP)) k_attn_dq(AttnArgs a) {
   }
 }
 
-// g_bias of head h: the workgroups' partials in order, a run per group of threads (8 to 64, as many as there are buckets), then the runs
-__device__ __forceinline__ void bias_reduce(const AttnArgs& a, int h, float* sh) {
+// g_bias of head h: the workgroups' partials in order, a run per group of threads (8 to 64, as many as there are buckets), then the runs, in
+// double precision: a bucket's partials nearly cancel (20,000 atoms: to 3e-4 of the sum of |ds|)
+__device__ __forceinline__ void bias_reduce(const AttnArgs& a, int h, double* sh) {
   const int w = a.nb <= 8 ? 8 : a.nb <= 16 ? 16 : a.nb <= 32 ? 32 : 64;
   const int b = threadIdx.x & (w - 1), run = threadIdx.x / w, runs = blockDim.x / w;
   const int per = (a.per_head + runs - 1) / runs, k1 = min(a.per_head, (run + 1) * per);
-  float s = 0.f;
+  double s = 0.0;
   if (b < a.nb) {
     const float* p = a.partial + (size_t)h * a.per_head * a.nb + b;
     for (int k = run * per; k < k1; k += 32) {   // 32 loads on their way at a time: the chain of their waits is the kernel's on small batches
@@ -882,8 +885,8 @@ __device__ __forceinline__ void bias_reduce(const AttnArgs& a, int h, float* sh)
   __syncthreads();
   if (run == 0 && b < a.nb) {
     for (int k = 1; k < runs; ++k) s += sh[k * w + b];
-    if (a.bias[(size_t)h * a.nb + b] == -__builtin_inff()) s = 0.f;   // its pairs are left out
-    a.g_bias[(size_t)h * a.nb + b] = s;
+    if (a.bias[(size_t)h * a.nb + b] == -__builtin_inff()) s = 0.0;   // its pairs are left out
+    a.g_bias[(size_t)h * a.nb + b] = (float)s;
   }
 }
 
@@ -895,7 +898,7 @@ __global__ void __launch_bounds__(256, DP == 128 || (!BF && DP == 64) ? 1 : 2) k
   constexpr int PT = Row<BF, 32>::PITCH;
   extern __shared__ __align__(16) char smem[];
   if ((int)blockIdx.x < a.nh) {   // uniform over the workgroup
-    bias_reduce(a, blockIdx.x, reinterpret_cast<float*>(smem));
+    bias_reduce(a, blockIdx.x, reinterpret_cast<double*>(smem));
     return;
   }
   const int lane = threadIdx.x & 63, wave = SPLIT ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0, g = lane >> 5;

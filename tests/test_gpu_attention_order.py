@@ -110,3 +110,33 @@ def test_captured_where_a_workgroup_takes_more_than_64_kb(dtype):
         assert all(torch.equal(a, w) for a, w in zip(res, want))
         both()
         torch.cuda.synchronize()
+
+
+def test_long_sums_of_the_bias_gradient():
+    """All pairs of the last bucket have one and the same ds, c, of 24 bits: a lane that added its 2,048 one after the other would be off by
+    the same rounding again and again. One key of 16,384 has a value, v; equal weights: p = 2^-14, D = v / 16384, c = -v 2^-28, all exact."""
+    import torch
+    from paper_2506_21788_amd import binding as B
+    n, d, nb, v = 16384, 8, 3, np.float32(1.5555555)
+    c = np.float32(v * np.float32(2.0 ** -28))
+    one = np.float32(0.0)
+    for _ in range(2048):
+        one = np.float32(one + c)
+    # a tile's sixteen, 128 tiles of a wavefront, the other half, 32 columns in eight chains, four wavefronts, the result's own rounding
+    allowed = (16 + 128 + 2 + 4 + 3 + 4 + 1) * U32
+    assert abs(float(one) / (2048 * float(c)) - 1.0) > 1.5 * allowed, "a chain of 2,048 would not show"
+    plan = torch.empty(B.pair_plan_workspace_bytes(n, 1), dtype=torch.uint8, device="cuda")
+    size = B.pair_plan(n, 1, dev(np.array([0, n]), "i32"), plan)
+    pairs = torch.full((size,), 2, dtype=torch.uint8, device="cuda")
+    pairs.view(n, n)[:, 0] = 0
+    qkv, g, bias = torch.zeros((n, 3, d), device="cuda"), torch.zeros((n, 1, d), device="cuda"), torch.zeros((1, nb), device="cuda")
+    qkv[0, 2, 0], g[:, 0, 0] = float(v), 1.0
+    ws_b, saved_b = B.graph_attention_workspace_bytes(n, 1, 1, 1, d, nb, B.F32)
+    ws, saved = (torch.empty(k, dtype=torch.uint8, device="cuda") for k in (ws_b, saved_b))
+    out, g_qkv, g_bias = torch.empty_like(g), torch.empty_like(qkv), torch.empty_like(bias)
+    B.graph_attention_fwd(n, 1, 1, 1, d, nb, B.F32, 1.0, plan, pairs, qkv, bias, out, saved)
+    B.graph_attention_bwd(n, 1, 1, 1, d, nb, B.F32, 1.0, plan, pairs, qkv, bias, out, saved, g, g_qkv, g_bias, ws)
+    got = g_bias.double().cpu().numpy()[0]
+    assert (out[:, 0, 0] == float(v) / n).all()
+    want = np.array([n * 2.0 ** -14 * (float(v) - float(v) / n), 0.0, -n * (n - 1) * float(c)])
+    assert (np.abs(got - want) <= allowed * np.abs(want)).all(), np.abs(got / np.where(want == 0, 1, want) - 1) / allowed
