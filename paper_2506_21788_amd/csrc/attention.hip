@@ -98,6 +98,10 @@ struct Row<true, DP> {
 #pragma unroll
     for (int k = 0; k < DP / 16; ++k) f[k] = *reinterpret_cast<const u32x4_t*>(tile + piece_at(row, 2 * k + g, PITCH));
   }
+  __device__ __forceinline__ void negate_if(bool yes) {
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k) f[k] ^= yes ? 0x80008000u : 0u;
+  }
   __device__ __forceinline__ static f32x16_t dot(const Row& a, const Row& b, f32x16_t acc) {
 #pragma unroll
     for (int k = 0; k < DP / 16; ++k)
@@ -141,6 +145,10 @@ struct Row<false, DP> {
       const float4 v = *reinterpret_cast<const float4*>(tile + row * PITCH + g * (DP / 2) + 4 * k);
       f[4 * k] = v.x; f[4 * k + 1] = v.y; f[4 * k + 2] = v.z; f[4 * k + 3] = v.w;
     }
+  }
+  __device__ __forceinline__ void negate_if(bool yes) {
+#pragma unroll
+    for (int s = 0; s < DP / 2; ++s) f[s] = yes ? -f[s] : f[s];
   }
   __device__ __forceinline__ static f32x16_t dot(const Row& a, const Row& b, f32x16_t acc) {
 #pragma unroll
@@ -705,6 +713,10 @@ __global__ void __launch_bounds__(256, dq_waves(BF, DP)) k_attn_dq(AttnArgs a) {
   const int hk = h / (a.nh / a.nkv);
   const unsigned ld = (unsigned)(a.nh + 2 * a.nkv) * a.dh, lo_ = (unsigned)a.nh * a.dh;
   const int ntiles = *a.plan.count;
+  // The matrix cores' sums of bf16 products are low by a hundredth of a step (6e-10 for 32 terms of size 1, measured), whatever their sign.
+  // In g_bias the rows would add that up (20,000 rows: 1.2e-5, half of its error), so every other wavefront works with -g and -D, and
+  // so with -ds, up to its sums.
+  const bool minus = ((wave ^ me) & 1) != 0;
 
   for (int t = me; t < ntiles; t += a.per_head) {   // uniform over the workgroup
     const Where w = tile_where(a, t);
@@ -739,6 +751,8 @@ __global__ void __launch_bounds__(256, dq_waves(BF, DP)) k_attn_dq(AttnArgs a) {
     if (!real) st = make_float2(0.f, __builtin_inff());
     if (real && g == 0 && wave == 0) a.delta[(size_t)h * a.N + w.lo + qi] = D;
     if (t == me) fill_table(table, my_bias, a.nb, a.inv, lane);
+    const float Ds = minus ? -D : D;
+    go.negate_if(minus);
     for (; j0 < w.n; j0 += step) {
       lds_order();
       kt.to_lds(tk, lane);
@@ -767,7 +781,7 @@ __global__ void __launch_bounds__(256, dq_waves(BF, DP)) k_attn_dq(AttnArgs a) {
       weights_of(s, a.c, st.x, st.y);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        ds[i] = s[i] * (ds[i] - D);
+        ds[i] = s[i] * (ds[i] - Ds);
         if (!LONG && i % HB == HB - 1) {
           hist_add(at, h2, ds, i - (HB - 1));
           if (i < 15) {
@@ -807,6 +821,10 @@ __global__ void __launch_bounds__(256, dq_waves(BF, DP)) k_attn_dq(AttnArgs a) {
         }
       }
       add_cols<BF, DP>(tk, Weights<BF>(ds), dq, lane);
+    }
+    if (minus) {
+#pragma unroll
+      for (int b = 0; b < DP / 32; ++b) dq[b] = -dq[b];
     }
     if constexpr (SPLIT) {
       static_assert(DP * 128 <= 2 * tile_bytes<BF, DP>(), "room for the join");
@@ -858,8 +876,10 @@ __global__ void __launch_bounds__(256, dq_waves(BF, DP)) k_attn_dq(AttnArgs a) {
   if constexpr (SPLIT) __syncthreads();
   if (wave == 0 && lane < a.nb) {
     float s = 0.f;
-    for (int k2 = 0; k2 < (SPLIT ? a.nw : 1); ++k2)
-      s += hist_sum<COLS>(reinterpret_cast<const float*>(smem + hist0 + k2 * wave_bytes), lane);
+    for (int k2 = 0; k2 < (SPLIT ? a.nw : 1); ++k2) {
+      const float x = hist_sum<COLS>(reinterpret_cast<const float*>(smem + hist0 + k2 * wave_bytes), lane);
+      s += (k2 ^ me) & 1 ? -x : x;
+    }
     a.partial[((size_t)h * a.per_head + me) * a.nb + lane] = s;
   }
 }

@@ -140,3 +140,27 @@ def test_long_sums_of_the_bias_gradient():
     assert (out[:, 0, 0] == float(v) / n).all()
     want = np.array([n * 2.0 ** -14 * (float(v) - float(v) / n), 0.0, -n * (n - 1) * float(c)])
     assert (np.abs(got - want) <= allowed * np.abs(want)).all(), np.abs(got / np.where(want == 0, 1, want) - 1) / allowed
+
+
+def test_bias_gradient_has_no_drift():
+    """The sum of g_bias for g_out and for -g_out: every rounding to nearest is the same for both but for its sign, so what is left is a drift of
+    the matrix cores' sums, which are low by some 6e-10 for 32 terms of size 1, whatever their sign. Rows must not add it up."""
+    import torch
+    from paper_2506_21788_amd import binding as B
+    n, d = 4096, 32
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    plan = torch.empty(B.pair_plan_workspace_bytes(n, 1), dtype=torch.uint8, device="cuda")
+    pairs = torch.zeros(B.pair_plan(n, 1, dev(np.array([0, n]), "i32"), plan), dtype=torch.uint8, device="cuda")
+    qkv = torch.zeros((n, 3, d), dtype=torch.bfloat16, device="cuda")
+    qkv[:, 2] = torch.randn((n, d), device="cuda", generator=gen).to(torch.bfloat16)
+    g = torch.randn((n, 1, d), device="cuda", generator=gen).to(torch.bfloat16)
+    bias = torch.zeros((1, 1), device="cuda")
+    ws_b, saved_b = B.graph_attention_workspace_bytes(n, 1, 1, 1, d, 1, B.BF16)
+    ws, saved = (torch.empty(k, dtype=torch.uint8, device="cuda") for k in (ws_b, saved_b))
+    out, g_qkv, both = torch.empty_like(g), torch.empty_like(qkv), [torch.empty_like(bias), torch.empty_like(bias)]
+    B.graph_attention_fwd(n, 1, 1, 1, d, 1, B.BF16, 1.0, plan, pairs, qkv, bias, out, saved)
+    for sign, res in zip((1.0, -1.0), both):
+        B.graph_attention_bwd(n, 1, 1, 1, d, 1, B.BF16, 1.0, plan, pairs, qkv, bias, out, saved, g * sign, g_qkv, res, ws)
+    drift = float(both[0].double() + both[1].double()) / (2 * n)
+    # a sixth of what one sum is low by; half a step of the two results, of size 1e-4 at most, is 1e-15 a row
+    assert abs(drift) <= 1e-10, drift
