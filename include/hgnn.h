@@ -415,7 +415,7 @@ int32_t hgnn_pair_buckets(void* stream, int32_t N, int32_t G, const void* plan, 
  * 1 <= nh <= 64, nkv divides nh, dh a multiple of 8 in 8..128, 1 <= nb <= 64, 1e-6 <= scale <= 1e6 (else BAD_SHAPE). N and G below 2^28, and
  * (N / 32 + min(N, G) + 64) nh below 2^26 (else OVERFLOW). Only enqueue work.
  * dtype HGNN_BF16 rounds p and ds to bfloat16 where they enter the products of g_q, g_k and g_v; out, g_bias and all softmax
- * statistics are formed without such a rounding.
+ * statistics are formed without such a rounding. Scores are float32, so a weight is off by a few 2^-24 of the larger of 1 and its score.
  * ------------------------------------------------------------------------------------------- */
 int32_t hgnn_graph_attention_workspace_bytes(int32_t N, int32_t G, int32_t nh, int32_t nkv, int32_t dh, int32_t nb, int32_t dtype,
                                              size_t* ws_bytes_host, size_t* saved_bytes_host);

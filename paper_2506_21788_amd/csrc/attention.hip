@@ -15,11 +15,12 @@
 // Operands that a product needs by columns go through LDS once, row by row, and come back through transposing reads (bf16)
 // or as single values (float32, matrix-core products of float32).
 //
-// Bound by the vector units. 20,000 atoms in one graph, 4 heads of 32, bf16: forward 0.88 ms (235 TFLOP/s), reverse 1.27 + 1.06 ms. Of
-// the 1,380 cycles that a tile of 1,024 scores takes a SIMD in k_attn_fwd, some 1,050 are vector instructions (exponentials
-// 256, the three terms of the weights 350, places in the table of biases 64), the matrix cores work for 256. In batches of small graphs
-// a wavefront has some four tiles, and its first loads and its end cost as much as two more: 390 graphs of 5 to 200 atoms,
-// 8 heads of 32 on 2, bf16, take 47 us forward (vector units 65 % busy) and 62 + 56 us in reverse (k_attn_dq: LDS 55, vector units 40 %).
+// Bound by the vector units forward, by waits in reverse. 20,000 atoms in one graph, 4 heads of 32, bf16: forward 0.83 ms (247 TFLOP/s),
+// reverse 1.17 + 0.97 ms. A tile of 1,024 scores takes a SIMD 1,110 cycles in k_attn_fwd, 79 % of them vector instructions (the three
+// terms of the weights 350, exponentials 128, places in the table of biases 64) and 23 % the matrix cores; 1,750 in k_attn_dq (vector units 56 %,
+// LDS 35, matrix cores 11) and 1,400 in k_attn_dkv (LDS 55, vector units 48, matrix cores 18) at 2.5 wavefronts a SIMD. In batches of small
+// graphs a wavefront has some four tiles, and its first loads and its end cost as much as two more: 390 graphs of 5 to 200 atoms,
+// 8 heads of 32 on 2, bf16, take 40 us forward (vector units 57 % busy) and 53 + 48 us in reverse (k_attn_dq: vector units 42 %, LDS 28).
 //
 // The sums of the reverse pass are split in two kernels (one owns queries, one keys) rather than added with atomics, so that
 // their order is fixed: the scores are formed twice. g_bias is collected in LDS, a column per lane and bucket (in long graphs lanes i and
@@ -1080,7 +1081,7 @@ bool long_graphs(int64_t G, int64_t N) { return N >= 1024 * G; }
 
 // Workgroups per head of k_attn_dq (each leaves one partial of g_bias): every tile its own while they are few, then as many as run
 // at once, which registers and LDS decide. (40,041 atoms in 390 graphs, 8 heads,
-// bf16: 62 us; 72 with a tenth more, 67 with half as many more, 72 with a workgroup per tile.) In long graphs, where a
+// bf16, in runs of 20 passes: 62 us; 72 with a tenth more, 67 with half as many more, 72 with a workgroup per tile.) In long graphs, where a
 // tile is a long chain, 4,096 and more are dealt out best.
 int64_t dq_per_head(int64_t max_tiles, int32_t N, int32_t G, int nh, int dh, int nb, bool bf16) {
   int64_t at_once = 4096;

@@ -9,7 +9,7 @@
 // float32 operands are staged as three bf16 terms and take six partial products (devmath.h): 2.7 times the rate of the float32
 // matrix cores at their precision. The forward pass keeps act'(z) in float32, so that the reverse pass multiplies by it where
 // it stages g_z: no tensor g_z exists. A bf16 call takes g_z = g_y act'(z) as two bf16 terms (terms_of_gz), 16 bits: one would add a rounding
-// to g_x's own and leave gW, a float32 result, with 8. (A third in gW takes 7 % more time for the reverse pass of 40,041 x 256 -> 512; with two
+// to g_x's own and leave gW, a float32 result, with 8. (A third in gW: both directions of 40,041 x 256 -> 512 take 7 % more time; with two
 // its error there is 2.5e-6, that of a float32 sum over the rows 2.2e-6.)
 //
 // The two products with W (large calls): W is laid out once per call in the order in which the matrix cores take it (k_pack), a 1 KB fragment
@@ -17,9 +17,9 @@
 // workgroup, half of the LDS traffic and of the splitting was W's, and the LDS was what bound the kernel (128 x 128 x 64:
 // 768 cycles of LDS against 512 of the matrix cores). The forward pass lays out W^T for the reverse pass as well, in `saved`.
 //
-// Bound by memory in bf16 (40,041 x 256 -> 512 with silu: 42 us forward, 40 and 36 in reverse, each moving 143 MB: 3.4 to 4.0 TB/s) and
-// by the matrix cores in float32 (7,703 x 866 -> 889 with gelu: 114, 104 and 97 us, six products of 11.9 GFLOP each:
-// 0.63 to 0.74 PFLOP/s, with the splitting on the vector units beside them).
+// Bound by memory in bf16 (40,041 x 256 -> 512 with silu: 37 us forward, 36 and 33 in reverse, each moving 143 MB: 3.8 to 4.4 TB/s) and
+// by waits in float32 (7,703 x 866 -> 889 with gelu: 96, 88 and 81 us, six products of 11.9 GFLOP each, 0.74 to 0.88 PFLOP/s: the matrix
+// cores are busy 32 to 37 % of the time, 1.2 to 1.5 wavefronts a SIMD wait half of theirs).
 //
 // Small calls (few tiles) take k_dense_small: 32 x 32 results, the contraction dealt to the four wavefronts of a workgroup, operands
 // straight from memory: nothing is staged, the chain is one load, some products and a join.

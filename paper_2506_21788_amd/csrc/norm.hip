@@ -5,7 +5,7 @@
 //     g_x = g',  g_s += g' gamma u,  g_z = g' s u gamma (1 - gamma),  q = g' s gamma,  g_w1 += q bh,  g_c1 += q,
 //     g_b = r1 (q w1 - [mean q w1] - bh mean(q w1 bh)),  g_w0 += g_y xh,  g_c0 += g_y.
 // Bound by memory: 14 bytes an element forward and 22 in reverse with bf16 blocks and a gate per channel (x, x', g 4 bytes each), a few
-// dozen operations. 40,041 x 256 in bf16: 30 and 49 us, 4.7 and 4.6 TB/s; 7,703 x 866 in float32: 25 and 38 us, 4.3 TB/s.
+// dozen operations. 40,041 x 256 in bf16: 29 and 48 us, 4.9 and 4.7 TB/s; 7,703 x 866 in float32: 24 and 37 us, 4.4 TB/s.
 // A row stays in the registers of LPR lanes of one wavefront (LPR = 16, 32 or 64 by the width), so every
 // tensor is read and written once and the sums of a row are lane exchanges; no shared memory, no barrier in the loop. The
 // reverse pass keeps the five parameter gradients of its columns in registers over all rows that a workgroup takes and leaves
