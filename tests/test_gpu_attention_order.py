@@ -164,3 +164,9 @@ def test_bias_gradient_has_no_drift():
     drift = float(both[0].double() + both[1].double()) / (2 * n)
     # a sixth of what one sum is low by; half a step of the two results, of size 1e-4 at most, is 1e-15 a row
     assert abs(drift) <= 1e-10, drift
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_graphs_of_one_atom_have_no_gradient_but_the_rounding(dtype):
+    """An atom that attends to itself alone: ds is what two float32 products of the same numbers differ by, and g_q and g_k no more than that."""
+    _check(_problem([1] * 700, 8, 4, 8, 2, dtype, holes=False))
