@@ -9,9 +9,8 @@ pytestmark = pytest.mark.gpu
 ACT = {"none": 0, "silu": 1, "gelu": 2}
 
 
-def _reverse(M, K, N, act, dtype, res, packed, bias=True, want_gx=True, gz_terms=3):
-    """Runs both directions and checks the gradients. packed: whether W^T has to be laid out for the reverse pass. gz_terms: bf16 terms
-    in which gW takes g_z."""
+def _reverse(M, K, N, act, dtype, res, packed):
+    """Runs both directions and checks the gradients. packed: whether W^T has to be laid out for the reverse pass."""
     import torch
     from paper_2506_21788_amd import binding as B
     print("dense reverse", M, K, N, act, dtype, res, flush=True)
@@ -27,7 +26,7 @@ def _reverse(M, K, N, act, dtype, res, packed, bias=True, want_gx=True, gz_terms
     y, g_x, gW, g_b = empty((M, N), dtype), empty((M, K), dtype), empty((K, N)), empty(N)
     dx, dW, dg = dev(x, dtype), dev(W, dtype), dev(g, dtype)
     B.dense_fwd(M, K, N, ACT[act], code, dx, dW, dev(b), None, y, saved, ws)
-    B.dense_bwd(M, K, N, ACT[act], code, dx, dW, saved, dg, g_x if want_gx else None, gW, g_b, ws, r_x=dev(rx, dtype) if want_gx else None)
+    B.dense_bwd(M, K, N, ACT[act], code, dx, dW, saved, dg, g_x, gW, g_b, ws, r_x=dev(rx, dtype))
     torch.cuda.synchronize()
     assert untouched(wg, sg)
     # z off by (K + 8) half-steps of float32 of its sum of magnitudes; act' by 0.8 of that (its slope) and 16 half-steps of its own
@@ -36,13 +35,12 @@ def _reverse(M, K, N, act, dtype, res, packed, bias=True, want_gx=True, gz_terms
     w_gx, w_gW, w_gb = ob.dense_bwd(x, W, b, act, g)
     gz = np.abs(g * d)
     egz = np.abs(g) * (0.8 * (K + 8) * U32 * zm + 16 * U32 * (1.0 + np.abs(z))) if act != "none" else np.zeros_like(gz)
-    # bf16: g_z enters g_x W^T as two terms, the second the rounded remainder of the first: 2^-8 twice, 2^-16 of it is lost at most
+    # bf16: g_z enters both products as two terms, the second the rounded remainder of the first: 2^-8 twice, 2^-16 of it is lost at most
     two = 2.0 ** -16 * gz if dtype == "bf16" and act != "none" else 0.0
-    if want_gx:
-        e = ((N + 8) * U32 * gz + egz + two) @ np.abs(W).T
-        want = w_gx + (0.0 if rx is None else rx)
-        close("g_x", g_x, want, e / U32 + np.abs(want), 1, dtype)
-    e = np.abs(x).T @ ((M + 8) * U32 * gz + egz + (two if gz_terms == 2 else 0.0))
+    e = ((N + 8) * U32 * gz + egz + two) @ np.abs(W).T
+    want = w_gx + (0.0 if rx is None else rx)
+    close("g_x", g_x, want, e / U32 + np.abs(want), 1, dtype)
+    e = np.abs(x).T @ ((M + 8) * U32 * gz + egz + two)
     close("gW", gW, w_gW, e / U32, 1)
     close("g_b", g_b, w_gb, (((M + 8) * U32 * gz + egz).sum(0)) / U32, 1)
 
@@ -51,4 +49,4 @@ def _reverse(M, K, N, act, dtype, res, packed, bias=True, want_gx=True, gz_terms
 @pytest.mark.parametrize("act,res", [("none", False), ("silu", True), ("gelu", False), ("none", True)])
 @pytest.mark.parametrize("M,K,N,packed", [(4200, 1030, 70, True), (16500, 200, 131, True), (1000, 650, 45, False), (33, 70, 35, False), (8100, 513, 301, True)])
 def test_g_x_keeps_g_z(M, K, N, packed, act, res, dtype):
-    _reverse(M, K, N, act, dtype, res, packed, gz_terms=2)
+    _reverse(M, K, N, act, dtype, res, packed)
